@@ -237,6 +237,89 @@ const char *lola_status_str(lola_status s);
  * MFMA kernel; "generic": shape-generic kernels.  which: 0 = lola_prefill, 1 = lola_decode_step. */
 const char *lola_kernel_path(const lola_config *cfg, int32_t which);
 
+/* ---- Softmax attention over the whole context, held in 8 bits ------------------------------------------------
+ *
+ * For the layers of a model that keep softmax attention, and as the other way of spending less memory on a context: a
+ * cache of up to `capacity` pairs per stream (sequence, kv head), keys and values as OCP e4m3 codes (4 exponent, 3 mantissa
+ * bits, largest 448) with one power-of-two scale for each block of LOLA_FULL_BLOCK slots and kv head, keys and values apart.
+ * lola_full_append quantises tokens into it, lola_full_attend is softmax attention over it, lola_full_step both for one
+ * token, lola_full_evict cuts it to the pairs that received the most attention.  The rules at the top of this file hold
+ * here too: caller-owned device memory, 16-byte alignment, everything that the host can know is checked before a launch, nothing
+ * synchronises, calls on one state or one workspace are ordered by the caller.  Every call may be captured into a graph.  Results
+ * depend on the arguments and the state alone: sums are taken in a fixed order. */
+enum { LOLA_FULL_BLOCK = 64 };
+
+typedef struct {
+    int32_t batch, n_q_heads, n_kv_heads;
+    int32_t head_dim;      /* d: 32, 64, 128 or 256 */
+    int32_t capacity;      /* slots per stream: a multiple of LOLA_FULL_BLOCK, at most 2^26 */
+    int32_t dtype;         /* LOLA_F32 | LOLA_BF16: storage type of q, k, v */
+    int32_t out_dtype;     /* LOLA_F32 | LOLA_BF16 */
+    int32_t tokens_first;  /* 0: q, out [B, Hq, T, d], k, v [B, Hkv, T, d]; 1: [B, T, Hq, d], [B, T, Hkv, d] */
+    float softmax_scale;   /* logit scale; <= 0 selects 1/sqrt(head_dim) */
+} lola_full_config;
+
+/* Slots at and beyond `count` hold nothing: whatever is in them is never read. */
+typedef struct {
+    uint8_t *k, *v;             /* [B, Hkv, capacity, d] codes; the value is code * scale of the slot's block */
+    float *k_scale, *v_scale;   /* [B, Hkv, capacity / LOLA_FULL_BLOCK] powers of two */
+    int32_t *idx;               /* [B, Hkv, capacity] token index of the pair in each slot (0 = the sequence's first token) */
+    float *weight;              /* [B, Hkv, capacity] attention weight that the pair has received; NULL: none is gathered */
+    int32_t *count;             /* [B, Hkv] slots in use */
+    int64_t *n_tokens;          /* [B, Hkv] tokens appended so far */
+} lola_full_state;
+
+/* Bytes of each state field in the order of the struct (host output, 8 entries); returns their sum, 0 if the
+ * configuration is invalid. */
+size_t lola_full_state_bytes(const lola_full_config *cfg, size_t field_bytes[8]);
+
+/* Workspace with which lola_full_attend of T tokens (gather as there; T = 1 also for lola_full_step) and lola_full_evict can
+ * be called; 0 if the configuration, T or gather is invalid.  Contents are scratch. */
+size_t lola_full_workspace_bytes(const lola_full_config *cfg, int32_t T, int32_t gather);
+
+/* Empty caches: count = 0, n_tokens = 0. */
+lola_status lola_full_init(const lola_full_config *cfg, const lola_full_state *st, void *stream);
+
+/*
+ * Appends T >= 0 tokens per sequence: k, v [B, Hkv, T, d] (or tokens first) go to slots count, count + 1, ..; idx =
+ * n_tokens, n_tokens + 1, ..; weight = 0; count and n_tokens grow.
+ * lens: NULL, or int32 [B]: of sequence b only the first lens[b] tokens exist (values outside 0 .. T count as the nearer end).
+ * Scales: e(a) is the least integer >= -100 with a <= 448 2^e.  A block that receives tokens gets the exponent
+ * e(largest magnitude among them), or, if it held tokens before, the larger of that and its own; codes it held are then
+ * rounded to it once more.  Codes are x 2^-e rounded to nearest even: within 2^-4 of the element, or 2^(e - 10) where
+ * that is more.
+ * A token with an element that is not finite is stored with NaN in place of its whole key, and zeros for those elements of its value:
+ * every query that sees it gets NaN, no other does.
+ * Tokens beyond `capacity` are not stored: count stays at capacity, n_tokens counts them.
+ */
+lola_status lola_full_append(const lola_full_config *cfg, const lola_full_state *st, const void *k, const void *v,
+                             const int32_t *lens, int32_t T, void *stream);
+
+/*
+ * Softmax attention of the newest tokens: with n = T, or lens[b], query i < n of a sequence is token n_tokens - n + i and sees
+ * the pairs whose idx is at most that.  All query heads of a group read the same cache:
+ *   y_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j) / sum_j exp(scale q_i.k_j).
+ * A query that sees nothing, and the rows i >= n, get zeros.
+ * gather = 1 adds sum over the group's query heads and i < n of p_ij to weight[j]; queries whose output is NaN add nothing.
+ * q, out [B, Hq, T, d] (or tokens first).  T >= 0; T * (Hq / Hkv) at most 2^24.
+ */
+lola_status lola_full_attend(const lola_full_config *cfg, const lola_full_state *st, const void *q, const int32_t *lens,
+                             int32_t T, int32_t gather, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One generation step: lola_full_append and lola_full_attend of one token per sequence, q, out [B, Hq, d], k, v [B, Hkv, d]. */
+lola_status lola_full_step(const lola_full_config *cfg, const lola_full_state *st, const void *q, const void *k, const void *v,
+                           int32_t gather, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Cuts every stream that holds more than `keep` pairs to `keep` (0 .. capacity; a larger value is refused): pairs with idx < first
+ * or idx >= n_tokens - recent stay (first, recent >= 0, first + recent <= keep), of the others those with the largest weight
+ * until there are `keep` (ties: the lower slot stays; NaN ranks above all numbers).  Pairs that stay keep their slots where those are
+ * below `keep`; the others, in ascending order, move into the slots below `keep` that became free, in ascending order, with weight and
+ * idx.  A block that receives pairs gets the larger of its exponent and the least that fits them, as in lola_full_append.
+ */
+lola_status lola_full_evict(const lola_full_config *cfg, const lola_full_state *st, int32_t keep, int32_t first, int32_t recent,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

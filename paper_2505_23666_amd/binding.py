@@ -20,7 +20,10 @@ LOLA_HIDE_STATE, LOLA_HIDE_SPARSE = 1, 2
 LOLA_SCORE_SRE, LOLA_SCORE_WERR_SQ, LOLA_SCORE_WERR_ABS, LOLA_SCORE_OVEREST, LOLA_SCORE_ATTN = 0, 1, 2, 3, 4
 EXPORTS = ("lola_state_bytes", "lola_prefill_workspace_bytes", "lola_state_init", "lola_state_flush", "lola_prefill",
            "lola_decode_step", "lola_status_str", "lola_kernel_path", "lola_release_streams", "lola_prefill_noalloc",
-           "lola_noalloc_scratch_bytes", "lola_step_scratch_bytes")
+           "lola_noalloc_scratch_bytes", "lola_step_scratch_bytes",
+           "lola_full_state_bytes", "lola_full_workspace_bytes", "lola_full_init", "lola_full_append", "lola_full_attend",
+           "lola_full_step", "lola_full_evict")
+LOLA_FULL_BLOCK = 64
 
 
 class LolaConfig(C.Structure):
@@ -34,6 +37,15 @@ class LolaState(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in (
         "H", "s", "win_k", "win_v", "sp_k", "sp_v", "sp_idx", "sp_count", "n_tokens",
         "pend_phi", "pend_v", "pend_count", "win_score", "sp_score")]
+
+
+class LolaFullConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in (
+        "batch", "n_q_heads", "n_kv_heads", "head_dim", "capacity", "dtype", "out_dtype", "tokens_first")] + [("softmax_scale", C.c_float)]
+
+
+class LolaFullState(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "idx", "weight", "count", "n_tokens")]
 
 
 class LolaError(RuntimeError):
@@ -74,6 +86,21 @@ def lib() -> C.CDLL:
         L.lola_prefill_noalloc.argtypes = [cfgp, stp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
         L.lola_noalloc_scratch_bytes.restype = sz
         L.lola_noalloc_scratch_bytes.argtypes = []
+        fcp, fsp = C.POINTER(LolaFullConfig), C.POINTER(LolaFullState)
+        L.lola_full_state_bytes.restype = sz
+        L.lola_full_state_bytes.argtypes = [fcp, C.POINTER(sz)]
+        L.lola_full_workspace_bytes.restype = sz
+        L.lola_full_workspace_bytes.argtypes = [fcp, i32, i32]
+        L.lola_full_init.restype = C.c_int
+        L.lola_full_init.argtypes = [fcp, fsp, vp]
+        L.lola_full_append.restype = C.c_int
+        L.lola_full_append.argtypes = [fcp, fsp, vp, vp, vp, i32, vp]
+        L.lola_full_attend.restype = C.c_int
+        L.lola_full_attend.argtypes = [fcp, fsp, vp, vp, i32, i32, vp, vp, sz, vp]
+        L.lola_full_step.restype = C.c_int
+        L.lola_full_step.argtypes = [fcp, fsp, vp, vp, vp, i32, vp, vp, sz, vp]
+        L.lola_full_evict.restype = C.c_int
+        L.lola_full_evict.argtypes = [fcp, fsp, i32, i32, i32, vp, sz, vp]
         L.lola_release_streams.restype = None
         L.lola_release_streams.argtypes = []
         _lib = L
@@ -139,6 +166,43 @@ def lola_release_streams() -> None:
 
 def lola_kernel_path(cfg: LolaConfig, which: int) -> str:
     return lib().lola_kernel_path(C.byref(cfg), which).decode()
+
+
+def lola_full_state_bytes(cfg: LolaFullConfig):
+    fb = (C.c_size_t * 8)()
+    tot = lib().lola_full_state_bytes(C.byref(cfg), fb)
+    return int(tot), [int(x) for x in fb]
+
+
+def lola_full_workspace_bytes(cfg: LolaFullConfig, T: int, gather: bool = False) -> int:
+    return int(lib().lola_full_workspace_bytes(C.byref(cfg), int(T), int(gather)))
+
+
+def _sized(t):
+    return _ptr(t), 0 if t is None else t.numel() * t.element_size()
+
+
+def lola_full_init(cfg: LolaFullConfig, st: LolaFullState) -> None:
+    _check(lib().lola_full_init(C.byref(cfg), C.byref(st), _stream()), "lola_full_init")
+
+
+def lola_full_append(cfg, st, k, v, lens, T) -> None:
+    _check(lib().lola_full_append(C.byref(cfg), C.byref(st), _ptr(k), _ptr(v), _ptr(lens), int(T), _stream()), "lola_full_append")
+
+
+def lola_full_attend(cfg, st, q, lens, T, gather, out, workspace) -> None:
+    _check(lib().lola_full_attend(C.byref(cfg), C.byref(st), _ptr(q), _ptr(lens), int(T), int(gather), _ptr(out), *_sized(workspace),
+                                  _stream()), "lola_full_attend")
+
+
+def lola_full_step(cfg, st, q, k, v, gather, out, workspace) -> None:
+    _check(lib().lola_full_step(C.byref(cfg), C.byref(st), _ptr(q), _ptr(k), _ptr(v), int(gather), _ptr(out), *_sized(workspace),
+                                _stream()), "lola_full_step")
+
+
+def lola_full_evict(cfg, st, keep, first, recent, workspace) -> None:
+    _check(lib().lola_full_evict(C.byref(cfg), C.byref(st), int(keep), int(first), int(recent), *_sized(workspace), _stream()),
+           "lola_full_evict")
 
 
 _TORCH_DT = {LOLA_F32: torch.float32, LOLA_BF16: torch.bfloat16}
@@ -242,3 +306,129 @@ class LolaLayer:
         with torch.cuda.device(self.device):
             lola_decode_step(self.cfg, self.st, q, k, v, Wq, Wk, out)
         return out
+
+
+class LolaFullCache:
+    """Device buffers of one layer's 8-bit full-context cache plus its calls (include/lola.h, lola_full_*).
+
+    capacity is rounded up to whole blocks of 64 slots.  buffers: the tensors of an existing cache by name (k, v float8_e4m3fn
+    [B, Hkv, capacity, d], k_scale, v_scale, idx, weight, count, n_tokens), used in place and not emptied; weights=False
+    leaves `weight` out: such a cache can neither gather weights nor evict."""
+
+    FIELDS = ("k", "v", "k_scale", "v_scale", "idx", "weight", "count", "n_tokens")
+
+    def __init__(self, B, Hq, Hkv, d, capacity, dtype="bf16", out_dtype="f32", scale=0.0, tokens_first=False, weights=True,
+                 buffers=None, device="cuda:0"):
+        self.device = torch.device(device)
+        cap = -(-int(capacity) // LOLA_FULL_BLOCK) * LOLA_FULL_BLOCK
+        self.dt = LOLA_BF16 if dtype == "bf16" else LOLA_F32
+        self.odt = LOLA_BF16 if out_dtype == "bf16" else LOLA_F32
+        self.cfg = LolaFullConfig(B, Hq, Hkv, d, cap, self.dt, self.odt, int(tokens_first), float(scale))
+        self.B, self.Hq, self.Hkv, self.d, self.capacity, self.tokens_first = B, Hq, Hkv, d, cap, bool(tokens_first)
+        tot, fb = lola_full_state_bytes(self.cfg)
+        if tot == 0:
+            raise LolaError("invalid configuration")
+        nb = cap // LOLA_FULL_BLOCK
+        shapes = {"k": ((B, Hkv, cap, d), torch.float8_e4m3fn), "v": ((B, Hkv, cap, d), torch.float8_e4m3fn),
+                  "k_scale": ((B, Hkv, nb), torch.float32), "v_scale": ((B, Hkv, nb), torch.float32),
+                  "idx": ((B, Hkv, cap), torch.int32), "weight": ((B, Hkv, cap), torch.float32),
+                  "count": ((B, Hkv), torch.int32), "n_tokens": ((B, Hkv), torch.int64)}
+        for name, (shape, dt) in shapes.items():
+            if buffers is not None:
+                t = buffers.get(name)
+                if t is not None and (t.shape != shape or t.dtype != dt or not t.is_contiguous() or t.device != self.device):
+                    raise LolaError(f"{name}: contiguous {dt} {shape} on {self.device} expected")
+                if t is None and name != "weight":
+                    raise LolaError(f"{name} is missing")
+            else:
+                t = torch.empty(shape, dtype=dt, device=self.device) if weights or name != "weight" else None
+            setattr(self, name, t)
+        fields = [getattr(self, n) for n in self.FIELDS]
+        assert [t.numel() * t.element_size() for t in fields if t is not None] == [b for b, t in zip(fb, fields) if t is not None]
+        self.st = LolaFullState(*[None if t is None else t.data_ptr() for t in fields])
+        self.workspace = None
+        self._ws_bytes = {}
+        self.fill = 0 if buffers is None else cap   # at least as many slots as any stream has in use
+        if buffers is None:
+            self.reset()
+
+    def reset(self):
+        """Empty caches."""
+        with torch.cuda.device(self.device):
+            lola_full_init(self.cfg, self.st)
+        self.fill = 0
+
+    def _ws(self, T, gather):
+        want = self._ws_bytes.get((T, gather))
+        if want is None:
+            want = self._ws_bytes[T, gather] = lola_full_workspace_bytes(self.cfg, T, gather)
+        if self.workspace is None or self.workspace.numel() < want:
+            self.workspace = torch.empty(max(want, 16), dtype=torch.uint8, device=self.device)
+        return self.workspace
+
+    def _room(self, T, lens):
+        """Raises where a sequence's tokens would not fit.  The counts are read back only when the host's own count of slots is
+        used up (never while a graph is captured: replays are the caller's to count)."""
+        if self.fill + T > self.capacity and not torch.cuda.is_current_stream_capturing():
+            new = T if lens is None else lens.clamp(0, T)[:, None]
+            if int((self.count + new).max()) > self.capacity:
+                raise LolaError(f"lola_full_append: the cache's {self.capacity} slots are used up: evict first")
+            self.fill = int(self.count.max())
+        self.fill = min(self.fill + T, self.capacity)
+
+    def _tokens(self, x, H, T=None):
+        if x.dtype != _TORCH_DT[self.dt] or x.device != self.device or not x.is_contiguous() or x.dim() != 4:
+            raise LolaError(f"contiguous {_TORCH_DT[self.dt]} with 4 dimensions on {self.device} expected")
+        n = x.shape[1] if self.tokens_first else x.shape[2]
+        if x.shape != ((self.B, n, H, self.d) if self.tokens_first else (self.B, H, n, self.d)) or (T is not None and n != T):
+            raise LolaError(f"tokens of {self.B} sequences, {H} heads, head_dim {self.d} expected, got {tuple(x.shape)}")
+        return n
+
+    def _lens(self, lens):
+        if lens is not None and (lens.shape != (self.B,) or lens.dtype != torch.int32 or lens.device != self.device or not lens.is_contiguous()):
+            raise LolaError(f"lens: contiguous int32 [{self.B}] on {self.device} expected")
+
+    def _out(self, out, shape):
+        if out is None:
+            return torch.empty(shape, dtype=_TORCH_DT[self.odt], device=self.device)
+        if out.shape != shape or out.dtype != _TORCH_DT[self.odt] or out.device != self.device or not out.is_contiguous():
+            raise LolaError(f"out: contiguous {_TORCH_DT[self.odt]} {tuple(shape)} on {self.device} expected")
+        return out
+
+    def append(self, k, v, lens=None):
+        """k, v [B, Hkv, T, d] ([B, T, Hkv, d] with tokens_first); lens int32 [B]: the sequences' own lengths, padded to T."""
+        T = self._tokens(k, self.Hkv)
+        self._tokens(v, self.Hkv, T)
+        self._lens(lens)
+        with torch.cuda.device(self.device):
+            self._room(T, lens)
+            lola_full_append(self.cfg, self.st, k, v, lens, T)
+
+    def attend(self, q, lens=None, out=None, gather=False):
+        """Outputs of the newest tokens' queries q [B, Hq, T, d] ([B, T, Hq, d]); gather adds their weights to `weight`."""
+        T = self._tokens(q, self.Hq)
+        self._lens(lens)
+        out = self._out(out, q.shape)
+        with torch.cuda.device(self.device):
+            lola_full_attend(self.cfg, self.st, q, lens, T, gather, out, self._ws(T, bool(gather)))
+        return out
+
+    def step(self, q, k, v, out=None, gather=False):
+        """append and attend of one token per sequence: q [B, Hq, d], k, v [B, Hkv, d]."""
+        want, dt = (self.B, self.Hkv, self.d), _TORCH_DT[self.dt]
+        if q.shape != (self.B, self.Hq, self.d) or k.shape != want or v.shape != want:
+            raise LolaError(f"q {(self.B, self.Hq, self.d)}, k and v {want} expected")
+        for x in (q, k, v):
+            if x.dtype != dt or x.device != self.device or not x.is_contiguous():
+                raise LolaError(f"contiguous {dt} on {self.device} expected")
+        out = self._out(out, q.shape)
+        with torch.cuda.device(self.device):
+            self._room(1, None)
+            lola_full_step(self.cfg, self.st, q, k, v, gather, out, self._ws(1, bool(gather)))
+        return out
+
+    def evict(self, keep, first=0, recent=0):
+        """Cut every stream to `keep` pairs: the first `first` and the most recent `recent` tokens, then those of largest weight."""
+        with torch.cuda.device(self.device):
+            lola_full_evict(self.cfg, self.st, keep, first, recent, self._ws(0, False))
+        self.fill = min(self.fill, keep)

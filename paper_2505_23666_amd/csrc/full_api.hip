@@ -1,0 +1,269 @@
+// C ABI of the 8-bit full-context cache (include/lola.h, lola_full_*): host-side validation, workspace carving and kernel
+// dispatch.  Nothing here allocates or synchronises.
+#include "../../include/lola.h"
+#include <algorithm>
+#include <math.h>
+#include "full_cache.h"
+
+using namespace lola;
+using namespace lola::full;
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+inline size_t up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+#define LAUNCH_CHECK() do { if (hipGetLastError() != hipSuccess) return LOLA_ERR_HIP; } while (0)
+
+lola_status check_config(const lola_full_config *c) {
+    if (!c) return LOLA_ERR_NULL;
+    if (c->dtype != LOLA_F32 && c->dtype != LOLA_BF16) return LOLA_ERR_DTYPE;
+    if (c->out_dtype != LOLA_F32 && c->out_dtype != LOLA_BF16) return LOLA_ERR_DTYPE;
+    if (c->batch < 1 || c->n_kv_heads < 1 || c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads) return LOLA_ERR_SHAPE;
+    if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return LOLA_ERR_SHAPE;
+    if (c->capacity < LOLA_FULL_BLOCK || c->capacity % LOLA_FULL_BLOCK || c->capacity > (1 << 26)) return LOLA_ERR_SHAPE;
+    // streams index the y dimension of some launch grids (limit 65535)
+    if ((long long)c->batch * c->n_kv_heads > 65535 || c->n_q_heads > 65535) return LOLA_ERR_SHAPE;
+    if (c->tokens_first != 0 && c->tokens_first != 1) return LOLA_ERR_SHAPE;
+    return LOLA_OK;
+}
+
+lola_status check_state(const lola_full_state *st) {
+    if (!st || !st->k || !st->v || !st->k_scale || !st->v_scale || !st->idx || !st->count || !st->n_tokens) return LOLA_ERR_NULL;
+    const void *ps[] = {st->k, st->v, st->k_scale, st->v_scale, st->idx, st->weight, st->count, st->n_tokens};
+    for (const void *p : ps) if (p && misaligned(p)) return LOLA_ERR_ALIGN;
+    return LOLA_OK;
+}
+
+bool rows_ok(const lola_full_config *c, int32_t T) {
+    return T >= 0 && (long long)T * (c->n_q_heads / c->n_kv_heads) <= (1 << 24);
+}
+
+Mem make_mem(const lola_full_state *st) {
+    return Mem{st->k, st->v, st->k_scale, st->v_scale, st->idx, st->weight, st->count, st->n_tokens};
+}
+
+Args make_args(const lola_full_config *c, const lola_full_state *st, int32_t T, const int32_t *lens) {
+    Args a = {};
+    a.mem = make_mem(st);
+    a.B = c->batch; a.Hq = c->n_q_heads; a.Hkv = c->n_kv_heads; a.g = a.Hq / a.Hkv;
+    a.d = c->head_dim; a.cap = c->capacity; a.nblk = a.cap / BLK; a.T = T;
+    a.lens = lens;
+    const int64_t d = a.d;
+    a.q_sb = (int64_t)a.Hq * T * d; a.k_sb = (int64_t)a.Hkv * T * d;
+    a.q_sh = c->tokens_first ? d : T * d; a.q_st = c->tokens_first ? a.Hq * d : d;
+    a.k_sh = a.q_sh; a.k_st = c->tokens_first ? a.Hkv * d : d;
+    a.scale2 = (c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / sqrtf((float)c->head_dim)) * LOG2E_F;
+    return a;
+}
+
+struct AttendPlan {
+    size_t off_stat, bytes;
+};
+AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
+    const size_t S = (size_t)c->batch * c->n_kv_heads, R = (size_t)T * (c->n_q_heads / c->n_kv_heads);
+    AttendPlan p;
+    size_t off = 0;
+    p.off_stat = off; if (gather) off += up(S * R * 2 * 4);
+    p.bytes = off;
+    return p;
+}
+
+struct EvictPlan {
+    size_t off_dst, off_src, off_before, off_edge, bytes;
+    int most, nkb;
+};
+EvictPlan plan_evict(const lola_full_config *c, int32_t keep) {
+    const size_t S = (size_t)c->batch * c->n_kv_heads;
+    EvictPlan p;
+    p.most = std::min(keep, c->capacity - keep);
+    p.nkb = (keep + BLK - 1) / BLK;
+    size_t off = 0;
+    p.off_dst = off; off += up(S * p.most * 4);
+    p.off_src = off; off += up(S * p.most * 4);
+    p.off_before = off; off += up(S * ((size_t)p.nkb + 1) * 4);
+    p.off_edge = off; off += up(S * 2 * 4);
+    p.bytes = off;
+    return p;
+}
+// an eviction to any budget: at most capacity / 2 pairs move, at most all blocks receive some
+size_t evict_bytes(const lola_full_config *c) {
+    const size_t S = (size_t)c->batch * c->n_kv_heads;
+    return 2 * up(S * (c->capacity / 2) * 4) + up(S * ((size_t)c->capacity / BLK + 1) * 4) + up(S * 2 * 4);
+}
+
+template <typename TI>
+lola_status run_append(const Args &a, hipStream_t stream) {
+    // blocks that T tokens may fall into; a workgroup takes both of a short call's, so that it can move the counters on itself
+    const int w = (int)(((int64_t)a.T + 2 * BLK - 2) / BLK), per = w <= 2 ? w : 1, adv = per == w;
+    const dim3 grid(a.B * a.Hkv, adv ? 1 : w);
+    switch (a.d) {
+        case 32: hipLaunchKernelGGL((append_kernel<32, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
+        case 64: hipLaunchKernelGGL((append_kernel<64, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
+        case 128: hipLaunchKernelGGL((append_kernel<128, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
+        default: hipLaunchKernelGGL((append_kernel<256, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
+    }
+    LAUNCH_CHECK();
+    if (!adv) {
+        hipLaunchKernelGGL(advance_kernel, dim3((a.B * a.Hkv + 255) / 256), dim3(256), 0, stream, a);
+        LAUNCH_CHECK();
+    }
+    return LOLA_OK;
+}
+
+template <int DH, typename TI, typename TO>
+lola_status launch_attend(const Args &a, float *stat, hipStream_t stream) {
+    const dim3 grid((a.T * a.g + 3) / 4, a.B * a.Hkv);
+    hipLaunchKernelGGL((attend_rows_kernel<DH, TI, TO>), grid, dim3(256), 0, stream, a, stat);
+    LAUNCH_CHECK();
+    if (stat) {
+        hipLaunchKernelGGL((gather_rows_kernel<DH, TI>), dim3(a.nblk, a.B * a.Hkv), dim3(256), 0, stream, a, stat);
+        LAUNCH_CHECK();
+    }
+    return LOLA_OK;
+}
+
+template <typename TI, typename TO>
+lola_status run_attend(const Args &a, float *stat, hipStream_t stream) {
+    switch (a.d) {
+        case 32: return launch_attend<32, TI, TO>(a, stat, stream);
+        case 64: return launch_attend<64, TI, TO>(a, stat, stream);
+        case 128: return launch_attend<128, TI, TO>(a, stat, stream);
+        default: return launch_attend<256, TI, TO>(a, stat, stream);
+    }
+}
+
+lola_status attend(const lola_full_config *c, const lola_full_state *st, const void *q, const int32_t *lens, int32_t T, int32_t gather,
+                   void *out, void *workspace, hipStream_t stream) {
+    Args a = make_args(c, st, T, lens);
+    a.q = q; a.out = out;
+    const AttendPlan p = plan_attend(c, T, gather);
+    float *stat = gather ? (float *)((char *)workspace + p.off_stat) : nullptr;
+    const bool bo = c->out_dtype == LOLA_BF16;
+    if (c->dtype == LOLA_F32) return bo ? run_attend<float, bf16_t>(a, stat, stream) : run_attend<float, float>(a, stat, stream);
+    return bo ? run_attend<bf16_t, bf16_t>(a, stat, stream) : run_attend<bf16_t, float>(a, stat, stream);
+}
+
+lola_status append(const lola_full_config *c, const lola_full_state *st, const void *k, const void *v, const int32_t *lens, int32_t T,
+                   hipStream_t stream) {
+    Args a = make_args(c, st, T, lens);
+    a.k = k; a.v = v;
+    return c->dtype == LOLA_F32 ? run_append<float>(a, stream) : run_append<bf16_t>(a, stream);
+}
+
+lola_status check_attend(const lola_full_config *c, const lola_full_state *st, const void *q, int32_t T, int32_t gather, const void *out,
+                         const void *workspace, size_t workspace_bytes) {
+    if (!q || !out || (gather && !st->weight)) return LOLA_ERR_NULL;
+    if (misaligned(q) || misaligned(out) || (workspace && misaligned(workspace))) return LOLA_ERR_ALIGN;
+    const size_t need = plan_attend(c, T, gather).bytes;
+    if (need && (!workspace || workspace_bytes < need)) return LOLA_ERR_WORKSPACE;
+    return LOLA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lola_full_state_bytes(const lola_full_config *c, size_t field_bytes[8]) {
+    if (check_config(c) != LOLA_OK) { if (field_bytes) std::fill(field_bytes, field_bytes + 8, (size_t)0); return 0; }
+    const size_t S = (size_t)c->batch * c->n_kv_heads, cap = c->capacity, codes = S * cap * c->head_dim, nb = S * (cap / BLK) * 4;
+    const size_t fb[8] = {codes, codes, nb, nb, S * cap * 4, S * cap * 4, S * 4, S * 8};
+    size_t total = 0;
+    for (int i = 0; i < 8; i++) { total += fb[i]; if (field_bytes) field_bytes[i] = fb[i]; }
+    return total;
+}
+
+size_t lola_full_workspace_bytes(const lola_full_config *c, int32_t T, int32_t gather) {
+    if (check_config(c) != LOLA_OK || !rows_ok(c, T) || (gather != 0 && gather != 1)) return 0;
+    return std::max(plan_attend(c, T, gather).bytes, evict_bytes(c));
+}
+
+lola_status lola_full_init(const lola_full_config *c, const lola_full_state *st, void *stream) {
+    lola_status rc = check_config(c);
+    if (rc != LOLA_OK) return rc;
+    rc = check_state(st);
+    if (rc != LOLA_OK) return rc;
+    const int S = c->batch * c->n_kv_heads;
+    hipLaunchKernelGGL(init_kernel, dim3((S + 255) / 256), dim3(256), 0, (hipStream_t)stream, st->count, st->n_tokens, S);
+    LAUNCH_CHECK();
+    return LOLA_OK;
+}
+
+lola_status lola_full_append(const lola_full_config *c, const lola_full_state *st, const void *k, const void *v,
+                             const int32_t *lens, int32_t T, void *stream) {
+    lola_status rc = check_config(c);
+    if (rc != LOLA_OK) return rc;
+    rc = check_state(st);
+    if (rc != LOLA_OK) return rc;
+    if (!rows_ok(c, T)) return LOLA_ERR_SHAPE;
+    if (T == 0) return LOLA_OK;   // nothing to read or write: the token pointers are not looked at
+    if (!k || !v) return LOLA_ERR_NULL;
+    if (misaligned(k) || misaligned(v) || (lens && misaligned(lens))) return LOLA_ERR_ALIGN;
+    return append(c, st, k, v, lens, T, (hipStream_t)stream);
+}
+
+lola_status lola_full_attend(const lola_full_config *c, const lola_full_state *st, const void *q, const int32_t *lens,
+                             int32_t T, int32_t gather, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    lola_status rc = check_config(c);
+    if (rc != LOLA_OK) return rc;
+    rc = check_state(st);
+    if (rc != LOLA_OK) return rc;
+    if (!rows_ok(c, T) || (gather != 0 && gather != 1)) return LOLA_ERR_SHAPE;
+    if (T == 0) return LOLA_OK;
+    rc = check_attend(c, st, q, T, gather, out, workspace, workspace_bytes);
+    if (rc != LOLA_OK) return rc;
+    if (lens && misaligned(lens)) return LOLA_ERR_ALIGN;
+    return attend(c, st, q, lens, T, gather, out, workspace, (hipStream_t)stream);
+}
+
+lola_status lola_full_step(const lola_full_config *c, const lola_full_state *st, const void *q, const void *k, const void *v,
+                           int32_t gather, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    lola_status rc = check_config(c);
+    if (rc != LOLA_OK) return rc;
+    rc = check_state(st);
+    if (rc != LOLA_OK) return rc;
+    if (!rows_ok(c, 1) || (gather != 0 && gather != 1)) return LOLA_ERR_SHAPE;
+    if (!k || !v) return LOLA_ERR_NULL;
+    rc = check_attend(c, st, q, 1, gather, out, workspace, workspace_bytes);
+    if (rc != LOLA_OK) return rc;
+    if (misaligned(k) || misaligned(v)) return LOLA_ERR_ALIGN;
+    rc = append(c, st, k, v, nullptr, 1, (hipStream_t)stream);
+    if (rc != LOLA_OK) return rc;
+    return attend(c, st, q, nullptr, 1, gather, out, workspace, (hipStream_t)stream);
+}
+
+lola_status lola_full_evict(const lola_full_config *c, const lola_full_state *st, int32_t keep, int32_t first, int32_t recent,
+                            void *workspace, size_t workspace_bytes, void *stream) {
+    lola_status rc = check_config(c);
+    if (rc != LOLA_OK) return rc;
+    rc = check_state(st);
+    if (rc != LOLA_OK) return rc;
+    if (keep < 0 || keep > c->capacity || first < 0 || recent < 0 || (long long)first + recent > keep) return LOLA_ERR_SHAPE;
+    if (!st->weight) return LOLA_ERR_NULL;
+    if (workspace && misaligned(workspace)) return LOLA_ERR_ALIGN;
+    if (keep == c->capacity) return LOLA_OK;   // no stream holds more
+    const EvictPlan p = plan_evict(c, keep);
+    if (!workspace || workspace_bytes < p.bytes) return LOLA_ERR_WORKSPACE;
+    EvictArgs a = {};
+    a.mem = make_mem(st);
+    a.cap = c->capacity; a.nblk = a.cap / BLK; a.keep = keep; a.first = first; a.recent = recent; a.d = c->head_dim;
+    char *ws = (char *)workspace;
+    a.dst = (int32_t *)(ws + p.off_dst); a.src = (int32_t *)(ws + p.off_src); a.before = (int32_t *)(ws + p.off_before);
+    a.edge = (float *)(ws + p.off_edge);
+    a.most = p.most; a.nkb = p.nkb;
+    const int S = c->batch * c->n_kv_heads;
+    hipLaunchKernelGGL(evict_select_kernel, dim3(S), dim3(1024), 0, (hipStream_t)stream, a);
+    LAUNCH_CHECK();
+    if (p.nkb == 0) return LOLA_OK;
+    const dim3 grid(p.nkb, S);
+    switch (a.d) {
+        case 32: hipLaunchKernelGGL((evict_move_kernel<32>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+        case 64: hipLaunchKernelGGL((evict_move_kernel<64>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+        case 128: hipLaunchKernelGGL((evict_move_kernel<128>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+        default: hipLaunchKernelGGL((evict_move_kernel<256>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+    }
+    LAUNCH_CHECK();
+    return LOLA_OK;
+}
+
+}  // extern "C"

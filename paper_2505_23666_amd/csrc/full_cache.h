@@ -1,0 +1,441 @@
+// Kernels of the 8-bit full-context cache (include/lola.h, lola_full_*): append, attention, eviction.
+//
+// One stream = one (sequence, kv head).  Codes are OCP e4m3, row-major [slot][d] for keys and values alike; a block of 64 slots
+// has one power-of-two scale for its keys and one for its values, so that quantising, rescaling and moving a code are exact up
+// to the single rounding to the e4m3 grid, and dequantising is exact.
+#pragma once
+#include "lola_common.h"
+
+namespace lola {
+namespace full {
+
+constexpr int BLK = 64;          // slots per block
+constexpr int EXP_MIN = -100;    // least exponent of a block's scale
+constexpr float LOG2E_F = 1.44269504088896340736f;
+
+struct Mem {
+    uint8_t *k, *v;
+    float *ks, *vs;
+    int32_t *idx;
+    float *weight;
+    int32_t *count;
+    int64_t *n_tokens;
+};
+
+struct Args {
+    Mem mem;
+    int B, Hq, Hkv, g, d, cap, nblk, T;
+    const int32_t *lens;
+    // token matrices: element offset of (b, head, token) is b * sb + head * sh + token * st
+    const void *q, *k, *v;
+    void *out;
+    int64_t q_sb, q_sh, q_st, k_sb, k_sh, k_st;
+    float scale2;                // logit scale * log2(e): softmax in powers of two
+};
+
+__device__ __forceinline__ int exponent_of(float scale) { return (int)((__float_as_uint(scale) >> 23) & 255u) - 127; }
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+// least e >= EXP_MIN with a <= 448 * 2^e, a >= 0 finite: 448 = 1.75 * 2^8, a = 1.f * 2^x (a below 2^-126 is below every bound)
+__device__ __forceinline__ int fit_exponent(float a) {
+    const uint32_t u = __float_as_uint(a);
+    const int x = (int)(u >> 23) - 127;
+    const int e = x - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return e < EXP_MIN ? EXP_MIN : e;
+}
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+// four floats -> four codes (round to nearest even; the callers' scales keep |x| <= 448)
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+__device__ __forceinline__ void from_codes(uint32_t c, float *x) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+    x[0] = lo[0]; x[1] = lo[1]; x[2] = hi[0]; x[3] = hi[1];
+}
+// codes of one block's scale -> codes of another's (f = 2^(old - new)); NaN stays
+__device__ __forceinline__ uint32_t rescale_codes(uint32_t c, float f) {
+    float x[4];
+    from_codes(c, x);
+    return to_codes(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+}
+
+__device__ __forceinline__ void load8(const float *p, float *x) {
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16_t *p, float *x) {
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u); }
+}
+
+__device__ __forceinline__ int new_tokens(const Args &a, int b) {
+    if (!a.lens) return a.T;
+    const int n = a.lens[b];
+    return n < 0 ? 0 : (n > a.T ? a.T : n);
+}
+__device__ __forceinline__ int held(const Args &a, int si) {
+    const int c = a.mem.count[si];
+    return c < 0 ? 0 : (c > a.cap ? a.cap : c);
+}
+
+// ---- append -------------------------------------------------------------------------------------------------
+// A workgroup takes `per` consecutive blocks of the window of blocks that a stream's new tokens fall into, one at a time: the
+// block's new rows (8 elements of a row per thread) are held in registers, the largest magnitudes are joined over the workgroup,
+// rows that the block held before are rescaled only if its exponent grows.  Bound by HBM: 2 T d elements read, 2 T d codes written.
+template <int DH, typename TI>
+__global__ __launch_bounds__(256) void append_kernel(Args a, int per, int advance) {
+    constexpr int TPR = DH / 8, RPP = 256 / TPR, NP = BLK / RPP < 1 ? 1 : BLK / RPP;   // threads per row, rows per pass, passes
+    __shared__ float red[2][4];
+    const int si = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int c0 = held(a, si), told = new_tokens(a, b), n = min(told, a.cap - c0);
+    const int64_t first = a.mem.n_tokens[si];
+    const TI *kp = (const TI *)a.k + b * a.k_sb + h * a.k_sh, *vp = (const TI *)a.v + b * a.k_sb + h * a.k_sh;
+    const int col = (tid % TPR) * 8, row0 = tid / TPR;
+    for (int i = 0; i < per; i++) {
+        const int J = c0 / BLK + blockIdx.y * per + i, lo = max(c0, J * BLK), hi = min(c0 + n, J * BLK + BLK);
+        if (lo >= hi) break;   // (uniform)
+        uint8_t *kc = a.mem.k + ((size_t)si * a.cap + (size_t)J * BLK) * DH, *vc = a.mem.v + ((size_t)si * a.cap + (size_t)J * BLK) * DH;
+        float x[NP][8], y[NP][8], ak = 0.f, av = 0.f;
+        bool bad[NP];
+#pragma unroll
+        for (int p = 0; p < NP; p++) {
+            const int slot = J * BLK + p * RPP + row0;
+            const bool mine = slot >= lo && slot < hi;
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[p][e] = y[p][e] = 0.f;
+            if (mine) {
+                load8(kp + (slot - c0) * a.k_st + col, x[p]);
+                load8(vp + (slot - c0) * a.k_st + col, y[p]);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < NP; p++) {
+            int nf = 0;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                if (!finite(x[p][e])) nf = 1;
+                if (!finite(y[p][e])) { nf = 1; y[p][e] = 0.f; }
+                av = fmaxf(av, fabsf(y[p][e]));
+            }
+#pragma unroll
+            for (int o = 1; o < TPR; o <<= 1) nf |= __shfl_xor(nf, o);
+            bad[p] = nf != 0;
+            if (!bad[p])
+#pragma unroll
+                for (int e = 0; e < 8; e++) ak = fmaxf(ak, fabsf(x[p][e]));
+        }
+        ak = wave_max(ak); av = wave_max(av);
+        __syncthreads();   // (the last block's readers are done)
+        if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
+        __syncthreads();
+        ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+        av = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+        int ek = fit_exponent(ak), ev = fit_exponent(av);
+        const int nold = max(0, c0 - J * BLK);   // rows held before
+        if (nold > 0) {
+            const int ok = exponent_of(a.mem.ks[(size_t)si * a.nblk + J]), ov = exponent_of(a.mem.vs[(size_t)si * a.nblk + J]);
+            ek = max(ek, ok); ev = max(ev, ov);
+            const float fk = pow2(max(ok - ek, -40)), fv = pow2(max(ov - ev, -40));   // (2^-40 takes every code to zero)
+            for (int e = tid; e < nold * TPR; e += 256) {
+                if (ek > ok) { uint2 u = reinterpret_cast<uint2 *>(kc)[e]; u.x = rescale_codes(u.x, fk); u.y = rescale_codes(u.y, fk); reinterpret_cast<uint2 *>(kc)[e] = u; }
+                if (ev > ov) { uint2 u = reinterpret_cast<uint2 *>(vc)[e]; u.x = rescale_codes(u.x, fv); u.y = rescale_codes(u.y, fv); reinterpret_cast<uint2 *>(vc)[e] = u; }
+            }
+            __syncthreads();   // every thread has read the old scales
+        }
+        if (tid == 0) { a.mem.ks[(size_t)si * a.nblk + J] = pow2(ek); a.mem.vs[(size_t)si * a.nblk + J] = pow2(ev); }
+        const float ik = pow2(-ek), iv = pow2(-ev);
+#pragma unroll
+        for (int p = 0; p < NP; p++) {
+            const int row = p * RPP + row0, slot = J * BLK + row;
+            if (slot < lo || slot >= hi) continue;
+            uint2 u;
+            u.x = to_codes(x[p][0] * ik, x[p][1] * ik, x[p][2] * ik, x[p][3] * ik);
+            u.y = to_codes(x[p][4] * ik, x[p][5] * ik, x[p][6] * ik, x[p][7] * ik);
+            if (bad[p]) u.x = u.y = 0x7F7F7F7Fu;
+            *reinterpret_cast<uint2 *>(kc + row * DH + col) = u;
+            u.x = to_codes(y[p][0] * iv, y[p][1] * iv, y[p][2] * iv, y[p][3] * iv);
+            u.y = to_codes(y[p][4] * iv, y[p][5] * iv, y[p][6] * iv, y[p][7] * iv);
+            *reinterpret_cast<uint2 *>(vc + row * DH + col) = u;
+        }
+        for (int s = lo + tid; s < hi; s += 256) {
+            a.mem.idx[(size_t)si * a.cap + s] = (int32_t)(first + (s - c0));
+            if (a.mem.weight) a.mem.weight[(size_t)si * a.cap + s] = 0.f;
+        }
+    }
+    if (advance) {   // this workgroup has all of the stream's blocks
+        __syncthreads();   // every thread has read count and n_tokens
+        if (tid == 0) { a.mem.count[si] = c0 + n; a.mem.n_tokens[si] = first + told; }
+    }
+}
+
+// count and n_tokens after an append of several workgroups per stream
+__global__ __launch_bounds__(256) void advance_kernel(Args a) {
+    const int si = blockIdx.x * 256 + threadIdx.x;
+    if (si >= a.B * a.Hkv) return;
+    const int c0 = held(a, si), told = new_tokens(a, si / a.Hkv);
+    a.mem.count[si] = c0 + min(told, a.cap - c0);
+    a.mem.n_tokens[si] += told;
+}
+
+__global__ __launch_bounds__(256) void init_kernel(int32_t *count, int64_t *n_tokens, int n) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) { count[i] = 0; n_tokens[i] = 0; }
+}
+
+// ---- attention, one wavefront per row -----------------------------------------------------------------------------
+// Row r = token * g + head of the group.  Lane l takes slot 64 J + l of a block for the logits and columns l, l + 64, .. of the output.
+template <int DH, typename TI, typename TO>
+__global__ __launch_bounds__(256) void attend_rows_kernel(Args a, float *stat) {
+    __shared__ __attribute__((aligned(16))) float q_l[4][DH];
+    constexpr int NC = DH / 64 < 1 ? 1 : DH / 64;
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, si = blockIdx.y, b = si / a.Hkv, h = si - b * a.Hkv;
+    const int R = a.T * a.g, r = blockIdx.x * 4 + w;
+    if (r >= R) return;   // (no workgroup barrier below)
+    const int t = r / a.g, hq = h * a.g + (r - t * a.g), n = new_tokens(a, b);
+    TO *op = (TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st;
+    const TI *qp = (const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st;
+    const int count = t < n ? held(a, si) : 0;
+    const int64_t pos = a.mem.n_tokens[si] - n + t;
+    if (count) for (int c = lane; c < DH; c += 64) q_l[w][c] = ldf(qp, c);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    float m = -INFINITY, l = 0.f, o[NC];
+#pragma unroll
+    for (int c = 0; c < NC; c++) o[c] = 0.f;
+    for (int J = 0; J * BLK < count; J++) {
+        const size_t row = (size_t)si * a.cap + (size_t)J * BLK;
+        const bool seen = J * BLK + lane < count && (int64_t)a.mem.idx[row + lane] <= pos;
+        float s = 0.f;
+        if (seen) {
+            const uint32_t *kc = reinterpret_cast<const uint32_t *>(a.mem.k + (row + lane) * DH);
+            for (int c = 0; c < DH / 4; c++) {
+                float x[4];
+                from_codes(kc[c], x);
+#pragma unroll
+                for (int e = 0; e < 4; e++) s = fmaf(x[e], q_l[w][4 * c + e], s);
+            }
+            s *= a.mem.ks[(size_t)si * a.nblk + J] * a.scale2;
+        } else s = -INFINITY;
+        const float mb = wave_max(s), mn = fmaxf(m, mb);
+        if (mn == -INFINITY && !__any(s != s)) continue;
+        const float f = m == -INFINITY ? 0.f : exp2f(m - mn);
+        const float p = seen ? exp2f(s - mn) : 0.f;
+        l = l * f + wave_sum(p);
+#pragma unroll
+        for (int c = 0; c < NC; c++) o[c] *= f;
+        const float vs = a.mem.vs[(size_t)si * a.nblk + J];
+        const int live = min(BLK, count - J * BLK);
+        for (int j = 0; j < live; j++) {
+            const float pj = __shfl(p, j) * vs;
+#pragma unroll
+            for (int c = 0; c < NC; c++) {
+                const int cc = lane + 64 * c;
+                if (cc < DH) { float x[4]; from_codes(a.mem.v[(row + j) * DH + cc], x); o[c] = fmaf(pj, x[0], o[c]); }
+            }
+        }
+        m = mn;
+    }
+    const float il = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int c = 0; c < NC; c++)
+        if (lane + 64 * c < DH) stf(op, lane + 64 * c, o[c] * il);
+    if (stat && lane == 0) {   // a row that saw nothing, or NaN, adds no weight
+        float *sp = stat + ((size_t)si * R + r) * 2;
+        sp[0] = m; sp[1] = (l > 0.f && finite(l)) ? 1.f / l : 0.f;
+    }
+}
+
+// weight[j] += sum over rows of exp2(s - m) / l: one workgroup per block of slots, a lane per slot, rows dealt to the wavefronts
+template <int DH, typename TI>
+__global__ __launch_bounds__(256) void gather_rows_kernel(Args a, const float *stat) {
+    __shared__ float sum_l[4][64];
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, si = blockIdx.y, J = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv;
+    const int count = held(a, si), n = new_tokens(a, b), R = a.T * a.g;
+    if (J * BLK >= count) return;
+    const size_t row = (size_t)si * a.cap + (size_t)J * BLK + lane;
+    const bool in = J * BLK + lane < count;
+    const int64_t at = in ? a.mem.idx[row] : 0, pos0 = a.mem.n_tokens[si] - n;
+    const float sc = a.mem.ks[(size_t)si * a.nblk + J] * a.scale2;
+    float acc = 0.f;
+    for (int r = w; r < n * a.g; r += 4) {
+        const int t = r / a.g, hq = h * a.g + (r - t * a.g);
+        const TI *qp = (const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st;
+        const float *sp = stat + ((size_t)si * R + r) * 2;
+        const float m = sp[0], il = sp[1];
+        if (il == 0.f || !in || at > pos0 + t) continue;
+        const uint32_t *kc = reinterpret_cast<const uint32_t *>(a.mem.k + row * DH);
+        float s = 0.f;
+        for (int c = 0; c < DH / 4; c++) {
+            float x[4];
+            from_codes(kc[c], x);
+#pragma unroll
+            for (int e = 0; e < 4; e++) s = fmaf(x[e], ldf(qp, 4 * c + e), s);
+        }
+        acc += exp2f(s * sc - m) * il;
+    }
+    sum_l[w][lane] = acc;
+    __syncthreads();
+    if (w == 0 && in) a.mem.weight[row] += (sum_l[0][lane] + sum_l[1][lane]) + (sum_l[2][lane] + sum_l[3][lane]);
+}
+
+// ---- eviction -------------------------------------------------------------------------------------------------
+struct EvictArgs {
+    Mem mem;
+    int cap, nblk, keep, first, recent, d;
+    // per stream: slots that become free, where their new pairs come from (ascending both), number of holes below each block,
+    // scales of the block that the budget ends in, as they were
+    int32_t *dst, *src, *before;
+    float *edge;
+    int most, nkb;               // entries per stream of dst and src; blocks that hold slots below keep
+};
+
+// larger rank = stays: pairs that always stay above all, then NaN, then by weight (any float, -0 = +0)
+__device__ __forceinline__ uint32_t rank_of(const EvictArgs &a, size_t at, int64_t recent_from) {
+    const int64_t i = a.mem.idx[at];
+    if (i < a.first || i >= recent_from) return 0xFFFFFFFFu;
+    const float w = a.mem.weight[at] + 0.f;
+    if (w != w) return 0xFFFFFFFEu;
+    const uint32_t u = __float_as_uint(w);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// exclusive sum over the workgroup's 1024 threads; *total receives the sum
+__device__ __forceinline__ int scan1024(int v, int *wsum, int *total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o); if (lane >= o) x += y; }
+    __syncthreads();
+    if (lane == 63) wsum[w] = x;
+    __syncthreads();
+    int base = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < 16; i++) { if (i < w) base += wsum[i]; all += wsum[i]; }
+    *total = all;
+    return base + x - v;
+}
+
+// One workgroup per stream: the keep-th largest rank by four passes over the ranks, eight bits each, then the lists.
+__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
+    __shared__ int hist[256], wsum[16], found[2];
+    const int si = blockIdx.x, tid = threadIdx.x;
+    int count = a.mem.count[si];
+    count = count < 0 ? 0 : (count > a.cap ? a.cap : count);
+    int32_t *before = a.before + (size_t)si * (a.nkb + 1);
+    if (count <= a.keep) {
+        for (int J = tid; J <= a.nkb; J += 1024) before[J] = 0;
+        return;
+    }
+    const size_t base = (size_t)si * a.cap;
+    const int64_t recent_from = a.mem.n_tokens[si] - a.recent;
+    uint32_t prefix = 0, mask = 0;
+    int want = a.keep;           // of the ranks that match the prefix, the want-th largest is looked for
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) hist[tid] = 0;
+        __syncthreads();
+        for (int s = tid; s < count; s += 1024) {
+            const uint32_t u = rank_of(a, base + s, recent_from);
+            if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255u], 1);
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int left = want, v = 255;
+            while (v > 0 && hist[v] < left) left -= hist[v--];
+            found[0] = v; found[1] = left;
+        }
+        __syncthreads();
+        prefix |= (uint32_t)found[0] << shift; mask |= 255u << shift; want = found[1];
+        __syncthreads();
+    }
+    // kept: rank > prefix, and the `want` lowest slots of those with rank == prefix
+    int ties = 0, holes = 0, moved = 0;
+    for (int s0 = 0; s0 < count; s0 += 1024) {
+        const int s = s0 + tid;
+        const uint32_t u = s < count ? rank_of(a, base + s, recent_from) : 0u;
+        int t_all, h_all, m_all;
+        const bool tie = s < count && u == prefix;
+        const int t_at = ties + scan1024(tie, wsum, &t_all);
+        const bool kept = s < count && (u > prefix || (tie && t_at < want));
+        const bool hole = s < a.keep && !kept, mover = s >= a.keep && kept;
+        const int h_at = holes + scan1024(hole, wsum, &h_all), m_at = moved + scan1024(mover, wsum, &m_all);
+        if (s < a.keep && s % BLK == 0) before[s / BLK] = h_at;
+        if (hole) a.dst[(size_t)si * a.most + h_at] = s;
+        if (mover) a.src[(size_t)si * a.most + m_at] = s;
+        ties += t_all; holes += h_all; moved += m_all;
+    }
+    if (tid == 0) {
+        before[a.nkb] = holes;
+        if (a.keep % BLK) {
+            a.edge[2 * si] = a.mem.ks[(size_t)si * a.nblk + a.keep / BLK];
+            a.edge[2 * si + 1] = a.mem.vs[(size_t)si * a.nblk + a.keep / BLK];
+        }
+        a.mem.count[si] = a.keep;
+    }
+}
+
+// One workgroup per block below the budget: the pairs that move into it come from slots at and beyond `keep`, which no workgroup writes.
+// (Of the block that the budget ends in only rows below it are rescaled; its scales, which other workgroups read as a
+// source's, are read from the copy taken beforehand.)
+template <int DH>
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
+    constexpr int TPR = DH / 8, RPP = 256 / TPR;
+    __shared__ float red[2][4];
+    const int si = blockIdx.y, J = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int j0 = a.before[(size_t)si * (a.nkb + 1) + J], j1 = a.before[(size_t)si * (a.nkb + 1) + J + 1];
+    if (j0 >= j1) return;
+    const int32_t *dst = a.dst + (size_t)si * a.most, *src = a.src + (size_t)si * a.most;
+    const size_t base = (size_t)si * a.cap;
+    const int col = (tid % TPR) * 8;
+    auto scale = [&](const float *p, int s, int which) {
+        return a.keep % BLK && s / BLK == a.keep / BLK ? a.edge[2 * si + which] : p[(size_t)si * a.nblk + s / BLK];
+    };
+    float ak = 0.f, av = 0.f;
+    for (int j = j0 + tid / TPR; j < j1; j += RPP) {
+        const int s = src[j];
+        const uint2 kc = *reinterpret_cast<const uint2 *>(a.mem.k + (base + s) * DH + col), vc = *reinterpret_cast<const uint2 *>(a.mem.v + (base + s) * DH + col);
+        float x[8], mk = 0.f, mv = 0.f;
+        from_codes(kc.x, x); from_codes(kc.y, x + 4);
+#pragma unroll
+        for (int e = 0; e < 8; e++) mk = fmaxf(mk, fabsf(x[e]));   // (a NaN key counts as zero)
+        from_codes(vc.x, x); from_codes(vc.y, x + 4);
+#pragma unroll
+        for (int e = 0; e < 8; e++) mv = fmaxf(mv, fabsf(x[e]));
+        ak = fmaxf(ak, mk * scale(a.mem.ks, s, 0));
+        av = fmaxf(av, mv * scale(a.mem.vs, s, 1));
+    }
+    ak = wave_max(ak); av = wave_max(av);
+    if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
+    const float ok_s = a.mem.ks[(size_t)si * a.nblk + J], ov_s = a.mem.vs[(size_t)si * a.nblk + J];
+    __syncthreads();
+    ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    av = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+    const int ok = exponent_of(ok_s), ov = exponent_of(ov_s), ek = max(ok, fit_exponent(ak)), ev = max(ov, fit_exponent(av));
+    uint8_t *kb = a.mem.k + (base + (size_t)J * BLK) * DH, *vb = a.mem.v + (base + (size_t)J * BLK) * DH;
+    if (ek > ok || ev > ov) {
+        const float fk = pow2(max(ok - ek, -40)), fv = pow2(max(ov - ev, -40));
+        const int rows = min(BLK, a.keep - J * BLK);
+        for (int e = tid; e < rows * TPR; e += 256) {
+            if (ek > ok) { uint2 u = reinterpret_cast<uint2 *>(kb)[e]; u.x = rescale_codes(u.x, fk); u.y = rescale_codes(u.y, fk); reinterpret_cast<uint2 *>(kb)[e] = u; }
+            if (ev > ov) { uint2 u = reinterpret_cast<uint2 *>(vb)[e]; u.x = rescale_codes(u.x, fv); u.y = rescale_codes(u.y, fv); reinterpret_cast<uint2 *>(vb)[e] = u; }
+        }
+        if (tid == 0) { a.mem.ks[(size_t)si * a.nblk + J] = pow2(ek); a.mem.vs[(size_t)si * a.nblk + J] = pow2(ev); }
+        __syncthreads();   // the rows that the moved pairs replace were rescaled by other threads
+    }
+    for (int j = j0 + tid / TPR; j < j1; j += RPP) {
+        const int s = src[j], t = dst[j];
+        uint2 kc = *reinterpret_cast<const uint2 *>(a.mem.k + (base + s) * DH + col), vc = *reinterpret_cast<const uint2 *>(a.mem.v + (base + s) * DH + col);
+        // (a source's exponent may be larger than the block's: its codes then grow, and fit by the choice of ek, ev)
+        const float fk = pow2(min(40, max(exponent_of(scale(a.mem.ks, s, 0)) - ek, -40))), fv = pow2(min(40, max(exponent_of(scale(a.mem.vs, s, 1)) - ev, -40)));
+        kc.x = rescale_codes(kc.x, fk); kc.y = rescale_codes(kc.y, fk);
+        vc.x = rescale_codes(vc.x, fv); vc.y = rescale_codes(vc.y, fv);
+        *reinterpret_cast<uint2 *>(a.mem.k + (base + t) * DH + col) = kc;
+        *reinterpret_cast<uint2 *>(a.mem.v + (base + t) * DH + col) = vc;
+        if (tid % TPR == 0) { a.mem.idx[base + t] = a.mem.idx[base + s]; a.mem.weight[base + t] = a.mem.weight[base + s]; }
+    }
+}
+
+}  // namespace full
+}  // namespace lola
