@@ -3,7 +3,7 @@
 #include "../../include/lola.h"
 #include <algorithm>
 #include <math.h>
-#include "full_cache.h"
+#include "full_step.h"
 
 using namespace lola;
 using namespace lola::full;
@@ -57,14 +57,31 @@ Args make_args(const lola_full_config *c, const lola_full_state *st, int32_t T, 
     return a;
 }
 
+constexpr int CHIP_CUS = 256;      // compute units of the MI355X
+// rows (query heads of a group x tokens) that the step kernel takes: two column tiles of 16, one where the head is 256 wide (two
+// would need more registers than there are)
+inline size_t step_rows(int head_dim) { return head_dim == 256 ? 16 : 32; }
+
 struct AttendPlan {
-    size_t off_stat, bytes;
+    bool step;
+    int nsplit;
+    size_t off_stat, off_o, off_ml, off_logit, bytes;
 };
 AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
     const size_t S = (size_t)c->batch * c->n_kv_heads, R = (size_t)T * (c->n_q_heads / c->n_kv_heads);
-    AttendPlan p;
+    AttendPlan p = {};
+    p.step = R <= step_rows(c->head_dim);
     size_t off = 0;
-    p.off_stat = off; if (gather) off += up(S * R * 2 * 4);
+    if (p.step) {
+        // four workgroups per compute unit; each wavefront of one has a block at least when the cache is full
+        const size_t most = ((size_t)c->capacity / BLK + STEP_NW - 1) / STEP_NW;
+        p.nsplit = (int)std::max((size_t)1, std::min(most, (4 * CHIP_CUS + S - 1) / S));
+        p.off_o = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * c->head_dim * 4);
+        p.off_ml = off; if (p.nsplit > 1 || gather) off += up(S * p.nsplit * R * 2 * 4);
+        p.off_logit = off; if (gather) off += up(S * R * c->capacity * 4);
+    } else {
+        p.off_stat = off; if (gather) off += up(S * R * 2 * 4);
+    }
     p.bytes = off;
     return p;
 }
@@ -112,7 +129,28 @@ lola_status run_append(const Args &a, hipStream_t stream) {
 }
 
 template <int DH, typename TI, typename TO>
-lola_status launch_attend(const Args &a, float *stat, hipStream_t stream) {
+lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *ws, hipStream_t stream) {
+    if (p.step) {
+        StepArgs sa;
+        sa.a = a; sa.nsplit = p.nsplit;
+        sa.part_o = p.nsplit > 1 ? (float *)(ws + p.off_o) : nullptr;
+        sa.part_ml = p.nsplit > 1 || gather ? (float *)(ws + p.off_ml) : nullptr;
+        sa.logit = gather ? (float *)(ws + p.off_logit) : nullptr;
+        const int S = a.B * a.Hkv, R = a.T * a.g;
+        const dim3 grid(S, p.nsplit);
+#define STEP(CT, M) hipLaunchKernelGGL((step_kernel<DH, CT, TI, TO, M>), grid, dim3(256), 0, stream, sa)
+        if (R <= 16) { if (a.T > 1) STEP(1, true); else STEP(1, false); }
+        else if constexpr (DH < 256) { if (a.T > 1) STEP(2, true); else STEP(2, false); }
+#undef STEP
+        LAUNCH_CHECK();
+        const int jo = p.nsplit > 1 ? (R * DH + 255) / 256 : 0, jw = gather ? std::min((a.cap + 255) / 256, 4096) : 0;
+        if (jo + jw) {
+            hipLaunchKernelGGL((step_join_kernel<DH, TO>), dim3(S, jo + jw), dim3(256), 0, stream, sa, jo);
+            LAUNCH_CHECK();
+        }
+        return LOLA_OK;
+    }
+    float *stat = gather ? (float *)(ws + p.off_stat) : nullptr;
     const dim3 grid((a.T * a.g + 3) / 4, a.B * a.Hkv);
     hipLaunchKernelGGL((attend_rows_kernel<DH, TI, TO>), grid, dim3(256), 0, stream, a, stat);
     LAUNCH_CHECK();
@@ -124,12 +162,12 @@ lola_status launch_attend(const Args &a, float *stat, hipStream_t stream) {
 }
 
 template <typename TI, typename TO>
-lola_status run_attend(const Args &a, float *stat, hipStream_t stream) {
+lola_status run_attend(const Args &a, const AttendPlan &p, int gather, char *ws, hipStream_t stream) {
     switch (a.d) {
-        case 32: return launch_attend<32, TI, TO>(a, stat, stream);
-        case 64: return launch_attend<64, TI, TO>(a, stat, stream);
-        case 128: return launch_attend<128, TI, TO>(a, stat, stream);
-        default: return launch_attend<256, TI, TO>(a, stat, stream);
+        case 32: return launch_attend<32, TI, TO>(a, p, gather, ws, stream);
+        case 64: return launch_attend<64, TI, TO>(a, p, gather, ws, stream);
+        case 128: return launch_attend<128, TI, TO>(a, p, gather, ws, stream);
+        default: return launch_attend<256, TI, TO>(a, p, gather, ws, stream);
     }
 }
 
@@ -138,10 +176,10 @@ lola_status attend(const lola_full_config *c, const lola_full_state *st, const v
     Args a = make_args(c, st, T, lens);
     a.q = q; a.out = out;
     const AttendPlan p = plan_attend(c, T, gather);
-    float *stat = gather ? (float *)((char *)workspace + p.off_stat) : nullptr;
+    char *ws = (char *)workspace;
     const bool bo = c->out_dtype == LOLA_BF16;
-    if (c->dtype == LOLA_F32) return bo ? run_attend<float, bf16_t>(a, stat, stream) : run_attend<float, float>(a, stat, stream);
-    return bo ? run_attend<bf16_t, bf16_t>(a, stat, stream) : run_attend<bf16_t, float>(a, stat, stream);
+    if (c->dtype == LOLA_F32) return bo ? run_attend<float, bf16_t>(a, p, gather, ws, stream) : run_attend<float, float>(a, p, gather, ws, stream);
+    return bo ? run_attend<bf16_t, bf16_t>(a, p, gather, ws, stream) : run_attend<bf16_t, float>(a, p, gather, ws, stream);
 }
 
 lola_status append(const lola_full_config *c, const lola_full_state *st, const void *k, const void *v, const int32_t *lens, int32_t T,

@@ -1,0 +1,336 @@
+// Attention of few rows over the 8-bit cache: the generation step, and calls of a few tokens (up to 32 rows, a row being one query of one
+// query head of the group).
+//
+// Bound by HBM: every code is read once for all rows of the group (256 bytes a slot at d = 128 against 2 x 4 x 128 x 2 flops for four heads).
+// A stream's blocks are dealt to `nsplit` workgroups and within one to its four wavefronts; each wavefront keeps a running maximum, sum
+// and output of its own over the blocks it reads, nothing is exchanged before its last block.
+//
+// One block (64 slots) of a wavefront:
+//   S^T = K Q^T   16x16x32 bf16: the codes are exact in bf16, so are bf16 queries; fp32 queries enter as three bf16 parts (24 bits).  A lane's
+//                 operand is eight consecutive bytes of its key row, straight from global memory: the order of the contraction
+//                 index is free as long as the queries are laid out the same.
+//   p = 2^(s - m + 14), rounded to fp16 (fp32 outputs: two fp16 parts): the operand of the second product.  The shift keeps weights down
+//                 to 2^-28 of the largest among fp16's normal numbers; the sum takes p before the rounding.
+//   O^T += V^T P^T  16x16x32 fp16: V's codes are exact in fp16 and are converted with their block's scale relative to the
+//                 largest so far; the codes pass through LDS for the transposing 8-bit read, 16-byte pieces XOR-swizzled
+//                 by row so that the 32 rows of a read meet all banks alike.  The C layout of the first product is the B layout of this one.
+#pragma once
+#include "full_cache.h"
+
+namespace lola {
+namespace full {
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef int i2 __attribute__((ext_vector_type(2)));
+
+constexpr int STEP_NW = 4;         // wavefronts per workgroup
+constexpr float P_SHIFT = 14.f;    // probabilities are held times 2^14
+
+// eight codes -> eight bf16 (exact)
+__device__ __forceinline__ bf8 codes_to_bf16(uint32_t a, uint32_t b) {
+    union { bf8 v; bf2 p[4]; } u;
+    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
+    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+    return u.v;
+}
+// eight codes times a power of two <= 1 -> eight fp16 (exact down to fp16's least number)
+__device__ __forceinline__ h8 codes_to_f16(uint32_t a, uint32_t b, float scale) {
+    union { h8 v; h2 p[4]; } u;
+    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, false); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, true);
+    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, false); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, true);
+    return u.v;
+}
+__device__ __forceinline__ i2 lds_read_tr8(const uint8_t *p) {
+    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i2 *)(p));
+}
+// x as NP bf16 parts whose sum it is (3 parts: 24 bits; bf16 inputs are their own first part)
+template <int NP>
+__device__ __forceinline__ void split_bf16(const float *x, bf8 *part) {
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) r[e] = x[e];
+#pragma unroll
+    for (int p = 0; p < NP; p++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const __bf16 h = (__bf16)r[e];
+            part[p][e] = h;
+            if (p + 1 < NP) r[e] = finite(r[e]) ? r[e] - (float)h : 0.f;
+        }
+}
+// (a product of NaN or infinite queries stays NaN or infinite through the first part alone)
+
+struct StepArgs {
+    Args a;
+    int nsplit;
+    float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
+    float *part_ml;    // [S][nsplit][R][2] running maximum (powers of two) and sum; sum 0: an empty share
+    float *logit;      // [S][R][cap] logits (powers of two) where weights are gathered, else NULL
+};
+
+// swizzle of the 16-byte pieces of an LDS row of DH bytes: rows whose addresses differ by a multiple of 256 bytes meet other banks
+template <int DH>
+__device__ __forceinline__ int vswz(int row) { return (row / (256 / DH)) & (DH / 16 - 1); }
+
+__device__ __forceinline__ float quad_max(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
+__device__ __forceinline__ float quad_sum(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+
+template <int DH, int CT, typename TI, typename TO, bool MASK>
+__global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
+    constexpr int QP = sizeof(TI) == 4 ? 3 : 1, PP = sizeof(TO) == 4 ? 2 : 1;
+    constexpr int NK = DH / 32;                     // contraction steps of the first product
+    constexpr int ND = DH / 16;                     // tiles of 16 output columns
+    constexpr int KB = DH / 4;                      // bytes of a key row per lane: quad q holds pieces c * 64 + q * 16 (DH = 32: q * 8)
+    constexpr int VI = DH / 16;                     // 16-byte loads per lane of a block's values
+    constexpr int PR = DH / 16;                     // pieces per row
+    __shared__ __attribute__((aligned(16))) uint8_t stage[STEP_NW][BLK * DH];
+    __shared__ float ml_l[STEP_NW][2][16 * CT], vref_l[STEP_NW];
+    const Args &a = sa.a;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
+    const int si = blockIdx.x, split = blockIdx.y, b = si / a.Hkv, h = si - b * a.Hkv;
+    const int R = a.T * a.g, n = new_tokens(a, b), count = n ? held(a, si) : 0;
+    const int nb = (count + BLK - 1) / BLK;
+    const int J0 = (int)((int64_t)nb * split / sa.nsplit), J1 = (int)((int64_t)nb * (split + 1) / sa.nsplit);
+    const uint8_t *kc = a.mem.k + (size_t)si * a.cap * DH, *vc = a.mem.v + (size_t)si * a.cap * DH;
+    const float *ks = a.mem.ks + (size_t)si * a.nblk, *vs = a.mem.vs + (size_t)si * a.nblk;
+    const int32_t *idx = a.mem.idx + (size_t)si * a.cap;
+    const int64_t pos0 = MASK ? a.mem.n_tokens[si] - n : 0;
+
+    uint32_t kr[4][KB / 4], vr[VI * 4];
+    float ksJ = 0.f, vsJ = 0.f;
+    int4 id[4];
+    auto load = [&](int J) {
+        const uint8_t *kp = kc + (size_t)J * BLK * DH, *vp = vc + (size_t)J * BLK * DH;
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const uint8_t *row = kp + (t * 16 + n16) * DH;
+            if constexpr (DH == 32) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(row + quad * 8);
+                kr[t][0] = u.x; kr[t][1] = u.y;
+            } else {
+#pragma unroll
+                for (int c = 0; c < DH / 64; c++) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(row + c * 64 + quad * 16);
+                    kr[t][4 * c] = u.x; kr[t][4 * c + 1] = u.y; kr[t][4 * c + 2] = u.z; kr[t][4 * c + 3] = u.w;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VI; i++) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(vp + i * 1024 + lane * 16);
+            vr[4 * i] = u.x; vr[4 * i + 1] = u.y; vr[4 * i + 2] = u.z; vr[4 * i + 3] = u.w;
+        }
+        ksJ = ks[J]; vsJ = vs[J];
+        if (MASK)
+#pragma unroll
+            for (int t = 0; t < 4; t++) id[t] = *reinterpret_cast<const int4 *>(idx + (size_t)J * BLK + t * 16 + quad * 4);
+    };
+    if (J0 + w < J1) load(J0 + w);
+
+    // queries of row 16 ct + n16 in the keys' order of columns
+    bf8 qf[CT][NK][QP];
+    int64_t pos[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ct++) {
+        const int r = ct * 16 + n16, t = r / a.g, hq = h * a.g + (r - t * a.g);
+        pos[ct] = pos0 + t;
+        const TI *qp = (const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st;
+#pragma unroll
+        for (int s = 0; s < NK; s++) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[e] = 0.f;
+            if (t < n) load8(qp + (DH == 32 ? quad * 8 : (s / 2) * 64 + quad * 16 + (s & 1) * 8), x);
+            split_bf16<QP>(x, qf[ct][s]);
+        }
+    }
+    f4 o[CT][ND];
+    float m[CT], l[CT], vref = 0.f;             // o is held in units of vref, the largest scale of values so far
+#pragma unroll
+    for (int ct = 0; ct < CT; ct++) {
+        m[ct] = -INFINITY; l[ct] = 0.f;
+#pragma unroll
+        for (int c = 0; c < ND; c++) o[ct][c] = (f4){0.f, 0.f, 0.f, 0.f};
+    }
+    uint8_t *st = stage[w];
+    for (int J = J0 + w; J < J1; J += STEP_NW) {
+        const int live = count - J * BLK;          // slots of this block that hold pairs (64 and more: all)
+        const float c = ksJ * a.scale2, vnew = fmaxf(vref, vsJ), vscale = vsJ / vnew, vkeep = vref / vnew;
+        vref = vnew;
+        // values to LDS; slots without a pair hold zeros there
+#pragma unroll
+        for (int i = 0; i < VI; i++) {
+            const int row = i * (64 / PR) + lane / PR, piece = lane % PR;
+            uint4 u = make_uint4(vr[4 * i], vr[4 * i + 1], vr[4 * i + 2], vr[4 * i + 3]);
+            if (row >= live) u = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>(st + row * DH + ((piece ^ vswz<DH>(row)) * 16)) = u;
+        }
+        f4 s[CT][4];
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ct++) s[ct][t] = (f4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NK; k++) {
+                const bf8 kf = codes_to_bf16(kr[t][2 * k], kr[t][2 * k + 1]);
+#pragma unroll
+                for (int ct = 0; ct < CT; ct++)
+#pragma unroll
+                    for (int p = QP - 1; p >= 0; p--) s[ct][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ct][k][p], s[ct][t], 0, 0, 0);
+            }
+        }
+        const int4 idJ[4] = {id[0], id[1], id[2], id[3]};
+        if (J + STEP_NW < J1) load(J + STEP_NW);
+        h8 pf[CT][2][PP];
+#pragma unroll
+        for (int ct = 0; ct < CT; ct++) {
+            float mb = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; t++) {
+                const int ids[4] = {idJ[t].x, idJ[t].y, idJ[t].z, idJ[t].w};
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    float v = s[ct][t][e] * c;
+                    if (t * 16 + quad * 4 + e >= live || (MASK && (int64_t)ids[e] > pos[ct])) v = -INFINITY;
+                    s[ct][t][e] = v;
+                    mb = fmaxf(mb, v);
+                }
+            }
+            if (sa.logit && ct * 16 + n16 < R) {
+                float *lp = sa.logit + ((size_t)si * R + ct * 16 + n16) * a.cap + (size_t)J * BLK + quad * 4;
+#pragma unroll
+                for (int t = 0; t < 4; t++) *reinterpret_cast<f4 *>(lp + t * 16) = s[ct][t];
+            }
+            mb = quad_max(mb);
+            const float mn = fmaxf(m[ct], mb), mu = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m[ct] - mu);   // (m = -inf: 0)
+            m[ct] = mn;
+            float sum = 0.f;
+#pragma unroll
+            for (int t = 0; t < 4; t++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float p = __builtin_amdgcn_exp2f(s[ct][t][e] - (mu - P_SHIFT));
+                    sum += p;
+                    const _Float16 hi = (_Float16)p;
+                    pf[ct][t / 2][0][(t & 1) * 4 + e] = hi;
+                    if (PP == 2) pf[ct][t / 2][PP - 1][(t & 1) * 4 + e] = (_Float16)(p - (float)hi);
+                }
+            l[ct] = l[ct] * f + quad_sum(sum);
+#pragma unroll
+            for (int d = 0; d < ND; d++) o[ct][d] *= f * vkeep;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int i8 = n16 >> 1, row = k * 32 + (i8 & 4) * 4 + quad * 4 + (i8 & 3);
+#pragma unroll
+            for (int d = 0; d < ND; d++) {
+                const i2 u = lds_read_tr8(st + row * DH + ((d ^ vswz<DH>(row)) * 16) + (n16 & 1) * 8);
+                const h8 vf = codes_to_f16((uint32_t)u[0], (uint32_t)u[1], vscale);
+#pragma unroll
+                for (int ct = 0; ct < CT; ct++)
+#pragma unroll
+                    for (int p = PP - 1; p >= 0; p--) o[ct][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[ct][k][p], o[ct][d], 0, 0, 0);
+            }
+        }
+    }
+
+    // the four wavefronts' shares: O^T [column][row] in turn through the staging memory, weighted by their maxima
+    if (lane == 0) vref_l[w] = vref;
+    if (quad == 0)
+#pragma unroll
+        for (int ct = 0; ct < CT; ct++) { ml_l[w][0][ct * 16 + n16] = m[ct]; ml_l[w][1][ct * 16 + n16] = l[ct]; }
+    __syncthreads();
+#pragma unroll
+    for (int ct = 0; ct < CT; ct++) {
+        float *ol = reinterpret_cast<float *>(stage[0]);     // [wavefront][column][16 rows]
+        if (ct) __syncthreads();
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) ol[(w * DH + d * 16 + quad * 4 + e) * 16 + n16] = o[ct][d][e];
+        __syncthreads();
+        for (int e = tid; e < 16 * DH; e += 256) {
+            const int r16 = e / DH, col = e - r16 * DH, r = ct * 16 + r16;
+            if (r >= R) continue;
+            float M = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < STEP_NW; i++) M = fmaxf(M, ml_l[i][0][r]);
+            const float mu = M == -INFINITY ? 0.f : M;
+            float L = 0.f, f[STEP_NW], y = 0.f;
+#pragma unroll
+            for (int i = 0; i < STEP_NW; i++) {
+                f[i] = __builtin_amdgcn_exp2f(ml_l[i][0][r] - mu);
+                L += ml_l[i][1][r] * f[i];
+            }
+            const int t = r / a.g, hq = h * a.g + (r - t * a.g);
+            if (t >= n) L = 0.f;     // padding
+            if (L != 0.f) {
+                const float iL = 1.f / L;
+#pragma unroll
+                for (int i = 0; i < STEP_NW; i++) y += ol[(i * DH + col) * 16 + r16] * f[i] * iL * vref_l[i];
+            }
+            if (sa.nsplit == 1) stf((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st, col, y);
+            else sa.part_o[(((size_t)si * sa.nsplit + split) * R + r) * DH + col] = y;
+            if (sa.part_ml && col == 0) {
+                float *p = sa.part_ml + (((size_t)si * sa.nsplit + split) * R + r) * 2;
+                p[0] = M; p[1] = L;
+            }
+        }
+    }
+}
+
+// Joins the shares: workgroups [0, jo) of a stream write its outputs, 256 elements each; the others, where weights are gathered, add
+// sum over rows of 2^(logit - M) / L to the weights of 256 slots at a time.
+template <int DH, typename TO>
+__global__ __launch_bounds__(256) void step_join_kernel(StepArgs sa, int jo) {
+    const Args &a = sa.a;
+    constexpr float SCALE = 1.f / 16384.f;           // sums hold p times 2^14
+    __shared__ float M_l[32], L_l[32];
+    const int tid = threadIdx.x, si = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv, R = a.T * a.g, ns = sa.nsplit;
+    const float *ml = sa.part_ml + (size_t)si * ns * R * 2;
+    const int n = new_tokens(a, b), count = n ? held(a, si) : 0, y = blockIdx.y;
+    if (y >= jo && (y - jo) * 256 >= count) return;
+    // eight lanes per row look at the shares
+    {
+        const int r = tid >> 3, j = tid & 7;
+        float M = -INFINITY, L = 0.f;
+        if (r < R) {
+            for (int s = j; s < ns; s += 8) M = fmaxf(M, ml[(s * R + r) * 2]);
+            M = fmaxf(M, __shfl_xor(M, 1)); M = fmaxf(M, __shfl_xor(M, 2)); M = fmaxf(M, __shfl_xor(M, 4));
+            const float mu = M == -INFINITY ? 0.f : M;
+            for (int s = j; s < ns; s += 8) L += ml[(s * R + r) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(s * R + r) * 2] - mu);
+            L += __shfl_xor(L, 1); L += __shfl_xor(L, 2); L += __shfl_xor(L, 4);
+            if (j == 0) { M_l[r] = mu; L_l[r] = L; }
+        }
+    }
+    __syncthreads();
+    if (y < jo) {
+        const int e = y * 256 + tid;
+        if (e >= R * DH) return;
+        const int r = e / DH, col = e - r * DH, t = r / a.g, hq = h * a.g + (r - t * a.g);
+        const float mu = M_l[r], L = L_l[r];
+        float acc = 0.f;
+        for (int s = 0; s < ns; s++) {
+            const float ms = ml[(s * R + r) * 2], ls = ml[(s * R + r) * 2 + 1];
+            // (an empty share's maximum is -inf: weight 0; its outputs are zeros)
+            acc += sa.part_o[(((size_t)si * ns + s) * R + r) * DH + col] * (ls * __builtin_amdgcn_exp2f(ms - mu));
+        }
+        stf((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st, col, L == 0.f ? 0.f : acc / L);
+    } else {
+        for (int slot = (y - jo) * 256 + tid; slot < count; slot += (gridDim.y - jo) * 256) {
+            float acc = 0.f;
+            for (int r = 0; r < n * a.g; r++) {
+                const float L = L_l[r];
+                if (L > 0.f && finite(L)) acc += __builtin_amdgcn_exp2f(sa.logit[((size_t)si * R + r) * a.cap + slot] - M_l[r]) / (L * SCALE);
+            }
+            a.mem.weight[(size_t)si * a.cap + slot] += acc;
+        }
+    }
+}
+
+}  // namespace full
+}  // namespace lola
