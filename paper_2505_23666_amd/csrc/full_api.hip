@@ -3,7 +3,7 @@
 #include "../../include/lola.h"
 #include <algorithm>
 #include <math.h>
-#include "full_step.h"
+#include "full_prompt.h"
 
 using namespace lola;
 using namespace lola::full;
@@ -35,8 +35,9 @@ lola_status check_state(const lola_full_state *st) {
     return LOLA_OK;
 }
 
+// (2^31 query rows in all is also what one grid dimension of the prompt kernel takes)
 bool rows_ok(const lola_full_config *c, int32_t T) {
-    return T >= 0 && (long long)T * (c->n_q_heads / c->n_kv_heads) <= (1 << 24);
+    return T >= 0 && (long long)T * (c->n_q_heads / c->n_kv_heads) <= (1 << 24) && (long long)T * c->batch * c->n_q_heads < (1ll << 31);
 }
 
 Mem make_mem(const lola_full_state *st) {
@@ -62,10 +63,12 @@ constexpr int CHIP_CUS = 256;      // compute units of the MI355X
 // would need more registers than there are)
 inline size_t step_rows(int head_dim) { return head_dim == 256 ? 16 : 32; }
 
+constexpr int PROMPT_NW = 4;       // wavefronts (of 32 rows) per workgroup of the prompt kernel
+
 struct AttendPlan {
     bool step;
-    int nsplit;
-    size_t off_stat, off_o, off_ml, off_logit, bytes;
+    int nsplit, ntiles;
+    size_t off_stat, off_o, off_ml, off_logit, off_span, bytes;
 };
 AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
     const size_t S = (size_t)c->batch * c->n_kv_heads, R = (size_t)T * (c->n_q_heads / c->n_kv_heads);
@@ -80,7 +83,14 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
         p.off_ml = off; if (p.nsplit > 1 || gather) off += up(S * p.nsplit * R * 2 * 4);
         p.off_logit = off; if (gather) off += up(S * R * c->capacity * 4);
     } else {
-        p.off_stat = off; if (gather) off += up(S * R * 2 * 4);
+        p.ntiles = (int)((R + 32 * PROMPT_NW - 1) / (32 * PROMPT_NW));
+        // two workgroups fit a compute unit; fewer are split over the blocks, four blocks each at least when the cache is full
+        const size_t wgs = S * p.ntiles, most = std::max((size_t)1, (size_t)c->capacity / BLK / 4);
+        p.nsplit = (int)(wgs >= 2 * CHIP_CUS ? 1 : std::min(most, (2 * CHIP_CUS + wgs - 1) / wgs));
+        p.off_span = off; off += up(S * (c->capacity / BLK) * 8);
+        p.off_o = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * c->head_dim * 4);
+        p.off_ml = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * 2 * 4);
+        p.off_stat = off; if (gather) off += up(S * R * 4);
     }
     p.bytes = off;
     return p;
@@ -112,8 +122,9 @@ size_t evict_bytes(const lola_full_config *c) {
 template <typename TI>
 lola_status run_append(const Args &a, hipStream_t stream) {
     // blocks that T tokens may fall into; a workgroup takes both of a short call's, so that it can move the counters on itself
-    const int w = (int)(((int64_t)a.T + 2 * BLK - 2) / BLK), per = w <= 2 ? w : 1, adv = per == w;
-    const dim3 grid(a.B * a.Hkv, adv ? 1 : w);
+    // (grid y is limited to 65535)
+    const int w = (int)(((int64_t)a.T + 2 * BLK - 2) / BLK), per = w <= 2 ? w : (w + 32767) / 32768, adv = per == w;
+    const dim3 grid(a.B * a.Hkv, (w + per - 1) / per);
     switch (a.d) {
         case 32: hipLaunchKernelGGL((append_kernel<32, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
         case 64: hipLaunchKernelGGL((append_kernel<64, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
@@ -150,12 +161,27 @@ lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *
         }
         return LOLA_OK;
     }
-    float *stat = gather ? (float *)(ws + p.off_stat) : nullptr;
-    const dim3 grid((a.T * a.g + 3) / 4, a.B * a.Hkv);
-    hipLaunchKernelGGL((attend_rows_kernel<DH, TI, TO>), grid, dim3(256), 0, stream, a, stat);
+    PromptArgs pa;
+    pa.a = a; pa.nsplit = p.nsplit; pa.ntiles = p.ntiles;
+    pa.span = (int2 *)(ws + p.off_span);
+    pa.part_o = p.nsplit > 1 ? (float *)(ws + p.off_o) : nullptr;
+    pa.part_ml = p.nsplit > 1 ? (float *)(ws + p.off_ml) : nullptr;
+    pa.stat = gather ? (float *)(ws + p.off_stat) : nullptr;
+    const int S = a.B * a.Hkv, R = a.T * a.g;
+    constexpr int LDS = 4 * BLK * DH * 2;
+    hipLaunchKernelGGL(span_kernel, dim3(std::min((a.nblk + 3) / 4, 256), S), dim3(256), 0, stream, pa);
     LAUNCH_CHECK();
-    if (stat) {
-        hipLaunchKernelGGL((gather_rows_kernel<DH, TI>), dim3(a.nblk, a.B * a.Hkv), dim3(256), 0, stream, a, stat);
+    hipLaunchKernelGGL((prompt_kernel<DH, PROMPT_NW, TI, TO>), dim3((unsigned)S * p.ntiles * p.nsplit), dim3(64 * PROMPT_NW), LDS, stream, pa);
+    LAUNCH_CHECK();
+    if (p.nsplit > 1) {
+        constexpr int RPW = 1024 / DH;      // rows per workgroup
+        hipLaunchKernelGGL((prompt_join_kernel<DH, TO>), dim3((R + RPW - 1) / RPW, S), dim3(256), 0, stream, pa);
+        LAUNCH_CHECK();
+    }
+    if (gather) {
+        // (a grid of 2^22 workgroups at most; each then takes several blocks)
+        const int nj = std::min(a.nblk, std::max(1, (1 << 22) / S));
+        hipLaunchKernelGGL((prompt_gather_kernel<DH, TI>), dim3((unsigned)S * nj), dim3(256), 0, stream, pa);
         LAUNCH_CHECK();
     }
     return LOLA_OK;

@@ -186,101 +186,6 @@ __global__ __launch_bounds__(256) void init_kernel(int32_t *count, int64_t *n_to
     if (i < n) { count[i] = 0; n_tokens[i] = 0; }
 }
 
-// ---- attention, one wavefront per row -----------------------------------------------------------------------------
-// Row r = token * g + head of the group.  Lane l takes slot 64 J + l of a block for the logits and columns l, l + 64, .. of the output.
-template <int DH, typename TI, typename TO>
-__global__ __launch_bounds__(256) void attend_rows_kernel(Args a, float *stat) {
-    __shared__ __attribute__((aligned(16))) float q_l[4][DH];
-    constexpr int NC = DH / 64 < 1 ? 1 : DH / 64;
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, si = blockIdx.y, b = si / a.Hkv, h = si - b * a.Hkv;
-    const int R = a.T * a.g, r = blockIdx.x * 4 + w;
-    if (r >= R) return;   // (no workgroup barrier below)
-    const int t = r / a.g, hq = h * a.g + (r - t * a.g), n = new_tokens(a, b);
-    TO *op = (TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st;
-    const TI *qp = (const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st;
-    const int count = t < n ? held(a, si) : 0;
-    const int64_t pos = a.mem.n_tokens[si] - n + t;
-    if (count) for (int c = lane; c < DH; c += 64) q_l[w][c] = ldf(qp, c);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    float m = -INFINITY, l = 0.f, o[NC];
-#pragma unroll
-    for (int c = 0; c < NC; c++) o[c] = 0.f;
-    for (int J = 0; J * BLK < count; J++) {
-        const size_t row = (size_t)si * a.cap + (size_t)J * BLK;
-        const bool seen = J * BLK + lane < count && (int64_t)a.mem.idx[row + lane] <= pos;
-        float s = 0.f;
-        if (seen) {
-            const uint32_t *kc = reinterpret_cast<const uint32_t *>(a.mem.k + (row + lane) * DH);
-            for (int c = 0; c < DH / 4; c++) {
-                float x[4];
-                from_codes(kc[c], x);
-#pragma unroll
-                for (int e = 0; e < 4; e++) s = fmaf(x[e], q_l[w][4 * c + e], s);
-            }
-            s *= a.mem.ks[(size_t)si * a.nblk + J] * a.scale2;
-        } else s = -INFINITY;
-        const float mb = wave_max(s), mn = fmaxf(m, mb);
-        if (mn == -INFINITY && !__any(s != s)) continue;
-        const float f = m == -INFINITY ? 0.f : exp2f(m - mn);
-        const float p = seen ? exp2f(s - mn) : 0.f;
-        l = l * f + wave_sum(p);
-#pragma unroll
-        for (int c = 0; c < NC; c++) o[c] *= f;
-        const float vs = a.mem.vs[(size_t)si * a.nblk + J];
-        const int live = min(BLK, count - J * BLK);
-        for (int j = 0; j < live; j++) {
-            const float pj = __shfl(p, j) * vs;
-#pragma unroll
-            for (int c = 0; c < NC; c++) {
-                const int cc = lane + 64 * c;
-                if (cc < DH) { float x[4]; from_codes(a.mem.v[(row + j) * DH + cc], x); o[c] = fmaf(pj, x[0], o[c]); }
-            }
-        }
-        m = mn;
-    }
-    const float il = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int c = 0; c < NC; c++)
-        if (lane + 64 * c < DH) stf(op, lane + 64 * c, o[c] * il);
-    if (stat && lane == 0) {   // a row that saw nothing, or NaN, adds no weight
-        float *sp = stat + ((size_t)si * R + r) * 2;
-        sp[0] = m; sp[1] = (l > 0.f && finite(l)) ? 1.f / l : 0.f;
-    }
-}
-
-// weight[j] += sum over rows of exp2(s - m) / l: one workgroup per block of slots, a lane per slot, rows dealt to the wavefronts
-template <int DH, typename TI>
-__global__ __launch_bounds__(256) void gather_rows_kernel(Args a, const float *stat) {
-    __shared__ float sum_l[4][64];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, si = blockIdx.y, J = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv;
-    const int count = held(a, si), n = new_tokens(a, b), R = a.T * a.g;
-    if (J * BLK >= count) return;
-    const size_t row = (size_t)si * a.cap + (size_t)J * BLK + lane;
-    const bool in = J * BLK + lane < count;
-    const int64_t at = in ? a.mem.idx[row] : 0, pos0 = a.mem.n_tokens[si] - n;
-    const float sc = a.mem.ks[(size_t)si * a.nblk + J] * a.scale2;
-    float acc = 0.f;
-    for (int r = w; r < n * a.g; r += 4) {
-        const int t = r / a.g, hq = h * a.g + (r - t * a.g);
-        const TI *qp = (const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st;
-        const float *sp = stat + ((size_t)si * R + r) * 2;
-        const float m = sp[0], il = sp[1];
-        if (il == 0.f || !in || at > pos0 + t) continue;
-        const uint32_t *kc = reinterpret_cast<const uint32_t *>(a.mem.k + row * DH);
-        float s = 0.f;
-        for (int c = 0; c < DH / 4; c++) {
-            float x[4];
-            from_codes(kc[c], x);
-#pragma unroll
-            for (int e = 0; e < 4; e++) s = fmaf(x[e], ldf(qp, 4 * c + e), s);
-        }
-        acc += exp2f(s * sc - m) * il;
-    }
-    sum_l[w][lane] = acc;
-    __syncthreads();
-    if (w == 0 && in) a.mem.weight[row] += (sum_l[0][lane] + sum_l[1][lane]) + (sum_l[2][lane] + sum_l[3][lane]);
-}
-
 // ---- eviction -------------------------------------------------------------------------------------------------
 struct EvictArgs {
     Mem mem;

@@ -1,0 +1,370 @@
+// Attention of many rows over the 8-bit cache: prompts, further turns, pieces of long prompts.  Row r of a stream is query
+// head r % g of token r / g: the heads of a group lie beside each other, so that a workgroup's rows cover few tokens and read one cache.
+//
+// One workgroup takes 32 NW rows of a stream, wavefront w the 32 from 32 w on, and goes over the blocks of 64 slots that any of them may
+// see; where there are few rows, the blocks are dealt to several workgroups and their shares joined.  A block's codes are loaded
+// into registers while the one before it is worked on, converted once for all rows and put into the other of two LDS buffers: keys as bf16, values as fp16
+// relative to the largest scale so far (both exact, up to fp16's range).  Products are 32x32x16 and transposed: S^T = K Q^T has a query per
+// lane pair, so the running maximum and sum live there, and its C layout is the B layout of O^T += V^T P^T, whose V^T comes from the
+// transposing 16-bit LDS read.  Which blocks can be passed over and which need a comparison per element follows from the least and largest token
+// index of each block, taken beforehand by a kernel of its own: slots need not be in the order of tokens (evictions fill holes).
+//
+// The maximum is only moved when a logit exceeds it by more than 2^RAISE: weights then reach 2^RAISE, held times 2^SHIFT in fp16.
+#pragma once
+#include "full_step.h"
+
+namespace lola {
+namespace full {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+
+constexpr float RAISE = 8.f, SHIFT = 7.f;
+
+struct PromptArgs {
+    Args a;
+    int nsplit, ntiles;
+    int2 *span;        // [S][nblk] least and largest token index of each block
+    float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
+    float *part_ml;    // [S][nsplit][R][2] maximum (powers of two) and sum
+    float *stat;       // [S][R] maximum + log2 of the sum (infinite: the row adds no weight), where weights are gathered
+};
+
+// least and largest token index of each block in use; slots without a pair count as later than all queries
+__global__ __launch_bounds__(256) void span_kernel(PromptArgs pa) {
+    const Args &a = pa.a;
+    const int si = blockIdx.y, lane = threadIdx.x & 63, count = held(a, si);
+    for (int J = blockIdx.x * 4 + (threadIdx.x >> 6); J * BLK < count; J += gridDim.x * 4) {
+        const int v = J * BLK + lane < count ? a.mem.idx[(size_t)si * a.cap + (size_t)J * BLK + lane] : 0x7FFFFFFF;
+        int lo = v, hi = v;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { lo = min(lo, __shfl_xor(lo, o)); hi = max(hi, __shfl_xor(hi, o)); }
+        if (lane == 0) pa.span[(size_t)si * a.nblk + J] = make_int2(lo, hi);
+    }
+}
+
+__device__ __forceinline__ h4 lds_read_tr16(const _Float16 *p) {
+    typedef __fp16 v4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) v4 *)(p)));
+}
+
+// swizzles of the 16-byte pieces of the rows in LDS (DH 2-byte numbers): 32 rows, one piece each (keys), and 4 rows x 64 bytes (values)
+template <int DH> __device__ __forceinline__ int kswz2(int row) { return DH >= 128 ? row & 15 : DH == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
+template <int DH> __device__ __forceinline__ int vswz2(int row) { return DH >= 128 ? (row & 3) << 2 : DH == 64 ? (row & 2) << 1 : 0; }
+
+__device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
+__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32); }
+
+template <int DH, int NW, typename TI, typename TO>
+__global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void prompt_kernel(PromptArgs pa) {
+    constexpr int QP = sizeof(TI) == 4 ? 3 : 1, PP = sizeof(TO) == 4 ? 2 : 1;
+    constexpr int NK = DH / 16, ND = DH / 32;           // contraction steps of S, tiles of 32 output columns
+    constexpr int NTHR = 64 * NW, TPR = DH / 16;        // threads per row of codes (16 each)
+    constexpr int NL = BLK * TPR / NTHR < 1 ? 1 : BLK * TPR / NTHR;   // 16-byte loads per thread
+    constexpr bool ALL = BLK * TPR >= NTHR;             // every thread loads
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two buffers of keys [64][DH] bf16 and values [64][DH] fp16
+    constexpr int HALF = BLK * DH * 2, BUF = 2 * HALF;
+    const Args &a = pa.a;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+    const int S = a.B * a.Hkv;
+    const int si = blockIdx.x % S, rest = blockIdx.x / S, split = rest % pa.nsplit, tile = pa.ntiles - 1 - rest / pa.nsplit;   // (long rows first)
+    const int b = si / a.Hkv, h = si - b * a.Hkv, R = a.T * a.g, n = new_tokens(a, b);
+    const int r0 = tile * 32 * NW, r = r0 + w * 32 + l32;
+    const int count = r0 < n * a.g ? held(a, si) : 0;
+    const int64_t pos0 = a.mem.n_tokens[si] - n;
+    const int t = r / a.g, hq = h * a.g + (r - t * a.g);
+    const int pos = (int)(pos0 + t);
+    const int64_t wg_last = pos0 + min((r0 + 32 * NW - 1) / a.g, n - 1);        // the workgroup's latest query
+    const int64_t w_first = pos0 + (r0 + w * 32) / a.g;                        // the wavefront's earliest
+    const uint8_t *kc = a.mem.k + (size_t)si * a.cap * DH, *vc = a.mem.v + (size_t)si * a.cap * DH;
+    const float *ks = a.mem.ks + (size_t)si * a.nblk, *vs = a.mem.vs + (size_t)si * a.nblk;
+    const int32_t *idx = a.mem.idx + (size_t)si * a.cap;
+    const int2 *span = pa.span + (size_t)si * a.nblk;
+    const int nb = (count + BLK - 1) / BLK;
+    const int J0 = (int)((int64_t)nb * split / pa.nsplit), J1 = (int)((int64_t)nb * (split + 1) / pa.nsplit);
+    auto next = [&](int J) { while (J < J1 && (int64_t)span[J].x > wg_last) J++; return J; };
+
+    bf8 qf[NK][QP];
+#pragma unroll
+    for (int s = 0; s < NK; s++) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = 0.f;
+        if (t < n) load8((const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st + s * 16 + hi * 8, x);
+        split_bf16<QP>(x, qf[s]);
+    }
+    f16v o[ND];
+#pragma unroll
+    for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) o[d][e] = 0.f;
+    float m = -INFINITY, l = 0.f;          // (l: this lane's half of the row)
+
+    uint4 kr[NL], vr[NL];
+    auto load = [&](int J) {
+        const uint8_t *kp = kc + (size_t)J * BLK * DH, *vp = vc + (size_t)J * BLK * DH;
+#pragma unroll
+        for (int i = 0; i < NL; i++)
+            if (ALL || tid < BLK * TPR) {
+                kr[i] = *reinterpret_cast<const uint4 *>(kp + (i * NTHR + tid) * 16);
+                vr[i] = *reinterpret_cast<const uint4 *>(vp + (i * NTHR + tid) * 16);
+            }
+    };
+    auto store = [&](uint8_t *buf, int J, float vscale) {
+        const int live = count - J * BLK;
+#pragma unroll
+        for (int i = 0; i < NL; i++)
+            if (ALL || tid < BLK * TPR) {
+                const int e = i * NTHR + tid, row = e / TPR, pc = (e % TPR) * 2;
+                uint8_t *kp = buf + row * DH * 2, *vp = buf + HALF + row * DH * 2;
+                *reinterpret_cast<bf8 *>(kp + ((pc ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].x, kr[i].y);
+                *reinterpret_cast<bf8 *>(kp + (((pc + 1) ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].z, kr[i].w);
+                if (row >= live) vr[i] = make_uint4(0, 0, 0, 0);      // slots without a pair hold zeros
+                *reinterpret_cast<h8 *>(vp + ((pc ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].x, vr[i].y, vscale);
+                *reinterpret_cast<h8 *>(vp + (((pc + 1) ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].z, vr[i].w, vscale);
+            }
+    };
+
+    int J = next(J0), cur = 0;
+    float vref = 0.f, vstage = 0.f;      // o is in units of vref; the staged block's values in units of vstage
+    if (J < J1) {
+        load(J);
+        vstage = vs[J];
+        store(lds, J, 1.f);
+    }
+    lds_barrier();
+    while (J < J1) {
+        const int Jn = next(J + 1);
+        const float c = ks[J] * a.scale2;
+        const bool masked = (int64_t)span[J].y > w_first;
+        if (Jn < J1) load(Jn);
+        const uint8_t *kb = lds + cur * BUF;
+        const _Float16 *vb = reinterpret_cast<const _Float16 *>(kb + HALF);
+        f16v s[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) s[kt][e] = 0.f;
+            const int row = kt * 32 + l32;
+#pragma unroll
+            for (int k = 0; k < NK; k++) {
+                const bf8 kf = *reinterpret_cast<const bf8 *>(kb + row * DH * 2 + (((2 * k + hi) ^ kswz2<DH>(row)) * 16));
+#pragma unroll
+                for (int p = QP - 1; p >= 0; p--) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k][p], s[kt], 0, 0, 0);
+            }
+        }
+        if (masked) {
+            const int live = count - J * BLK;
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const int at = kt * 32 + q * 8 + hi * 4;
+                    const int4 id = *reinterpret_cast<const int4 *>(idx + (size_t)J * BLK + at);
+                    const int ids[4] = {id.x, id.y, id.z, id.w};
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (at + e >= live || ids[e] > pos) s[kt][q * 4 + e] = -INFINITY;
+                }
+        }
+        float mb = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) mb = fmaxf(mb, s[kt][e]);
+        mb *= c;
+        if (__any(mb > m + RAISE || (m == -INFINITY && mb > m))) {
+            mb = half_max(mb);
+            const float mn = fmaxf(m, mb), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn; l *= f;
+#pragma unroll
+            for (int d = 0; d < ND; d++) o[d] *= f;
+        }
+        if (vstage > vref) {      // (uniform; rare beyond the first block)
+            const float f = vref / vstage;
+#pragma unroll
+            for (int d = 0; d < ND; d++) o[d] *= f;
+            vref = vstage;
+        }
+        const float off = (m == -INFINITY ? 0.f : m) - SHIFT;
+        h8 pf[4][PP];
+        float sum = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off));
+                sum += p;
+                const _Float16 ph = (_Float16)p;
+                pf[kt * 2 + e / 8][0][e & 7] = ph;
+                if (PP == 2) pf[kt * 2 + e / 8][PP - 1][e & 7] = (_Float16)(p - (float)ph);
+            }
+        l += sum;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int j = lane & 15, key = k * 16 + hi * 4 + (j >> 2);
+#pragma unroll
+            for (int d = 0; d < ND; d++) {
+                const int col = d * 32 + ((lane >> 4) & 1) * 16 + (j & 3) * 4;
+                h8 vf;
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    const int row = key + 8 * x;
+                    const h4 u = lds_read_tr16(vb + row * DH + (((col >> 3) ^ vswz2<DH>(row)) << 3) + (col & 7));
+                    vf[4 * x] = u[0]; vf[4 * x + 1] = u[1]; vf[4 * x + 2] = u[2]; vf[4 * x + 3] = u[3];
+                }
+#pragma unroll
+                for (int p = PP - 1; p >= 0; p--) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[k][p], o[d], 0, 0, 0);
+            }
+        }
+        if (Jn < J1) {
+            const float v = vs[Jn];
+            vstage = fmaxf(vstage, v);
+            store(lds + (cur ^ 1) * BUF, Jn, v / vstage);
+        }
+        lds_barrier();
+        J = Jn; cur ^= 1;
+    }
+    l = half_sum(l);
+    if (r < R) {
+        const bool pad = t >= n;
+        const float il = pad || l == 0.f ? 0.f : vref / l;
+        if (pa.nsplit == 1) {
+            TO *op = (TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st;
+#pragma unroll
+            for (int d = 0; d < ND; d++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) stf(op, d * 32 + (e / 4) * 8 + hi * 4 + (e & 3), il == 0.f ? 0.f : o[d][e] * il);
+            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = (!pad && l > 0.f && finite(l)) ? m + __builtin_amdgcn_logf(l) - SHIFT : INFINITY;
+        } else {
+            const size_t at = ((size_t)si * pa.nsplit + split) * R + r;
+            float *op = pa.part_o + at * DH;
+#pragma unroll
+            for (int d = 0; d < ND; d++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    f4 u;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) u[e] = il == 0.f ? 0.f : o[d][q * 4 + e] * il;
+                    *reinterpret_cast<f4 *>(op + d * 32 + q * 8 + hi * 4) = u;
+                }
+            if (hi == 0) { pa.part_ml[at * 2] = m; pa.part_ml[at * 2 + 1] = pad ? 0.f : l; }
+        }
+    }
+}
+
+// joins the shares of a row: DH / 4 threads each
+template <int DH, typename TO>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs pa) {
+    const Args &a = pa.a;
+    constexpr int TPR = DH / 4;
+    const int si = blockIdx.y, R = a.T * a.g, r = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, col = (threadIdx.x % TPR) * 4;
+    if (r >= R) return;
+    const int b = si / a.Hkv, h = si - b * a.Hkv, t = r / a.g, hq = h * a.g + (r - t * a.g);
+    float M = -INFINITY, L = 0.f;
+    for (int s = 0; s < pa.nsplit; s++) M = fmaxf(M, pa.part_ml[(((size_t)si * pa.nsplit + s) * R + r) * 2]);
+    const float mu = M == -INFINITY ? 0.f : M;
+    f4 acc = (f4){0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < pa.nsplit; s++) {
+        const size_t at = ((size_t)si * pa.nsplit + s) * R + r;
+        const float f = pa.part_ml[at * 2 + 1] * __builtin_amdgcn_exp2f(pa.part_ml[at * 2] - mu);
+        L += f;
+        acc += *reinterpret_cast<const f4 *>(pa.part_o + at * DH + col) * f;
+    }
+    TO *op = (TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st;
+#pragma unroll
+    for (int e = 0; e < 4; e++) stf(op, col + e, L == 0.f ? 0.f : acc[e] / L);
+    if (pa.stat && col == 0) pa.stat[(size_t)si * R + r] = (L > 0.f && finite(L)) ? mu + __builtin_amdgcn_logf(L) - SHIFT : INFINITY;
+}
+
+// weight[j] += sum over rows of 2^(logit - stat): one workgroup per block of slots, whose keys stay in registers as the first operand of
+// S^T = K Q^T; the wavefronts take 32 rows in turn, straight from global memory, and join their sums at the end
+template <int DH, typename TI>
+__global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void prompt_gather_kernel(PromptArgs pa) {
+    constexpr int QP = sizeof(TI) == 4 ? 3 : 1, NK = DH / 16;
+    __shared__ float sum_l[4][64];
+    const Args &a = pa.a;
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+    const int S = a.B * a.Hkv, si = blockIdx.x % S, b = si / a.Hkv, h = si - b * a.Hkv;
+    const int R = a.T * a.g, n = new_tokens(a, b), count = n ? held(a, si) : 0;
+    for (int J = blockIdx.x / S; J * BLK < count; J += gridDim.x / S) {
+        const int2 sp = pa.span[(size_t)si * a.nblk + J];
+        const int64_t pos0 = a.mem.n_tokens[si] - n;
+        const int live = count - J * BLK;
+        bf8 kf[2][NK];
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int k = 0; k < NK; k++) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(a.mem.k + ((size_t)si * a.cap + (size_t)J * BLK + kt * 32 + l32) * DH + k * 16 + hi * 8);
+                kf[kt][k] = codes_to_bf16(u.x, u.y);
+            }
+        int ids[2][16];
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+                const int at = kt * 32 + (e / 4) * 8 + hi * 4 + (e & 3);
+                ids[kt][e] = at < live ? a.mem.idx[(size_t)si * a.cap + (size_t)J * BLK + at] : 0x7FFFFFFF;
+            }
+        const float c = a.mem.ks[(size_t)si * a.nblk + J] * a.scale2;
+        float acc[2][16];
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) acc[kt][e] = 0.f;
+        // rows from the first token that sees any of the block's pairs
+        const int64_t t0 = (int64_t)sp.x > pos0 ? (int64_t)sp.x - pos0 : 0;
+        const int rows = n * a.g, first = t0 >= n ? rows : (int)t0 * a.g / 32 * 32;
+        for (int r0 = first + w * 32; r0 < rows; r0 += 128) {
+            const int r = r0 + l32, t = r / a.g, hq = h * a.g + (r - t * a.g);
+            const int pos = (int)(pos0 + t);
+            const float st = r < rows ? pa.stat[(size_t)si * R + r] : INFINITY;
+            f16v s[2];
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) s[kt][e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NK; k++) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] = 0.f;
+                if (r < rows) load8((const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st + k * 16 + hi * 8, x);
+                bf8 qf[QP];
+                split_bf16<QP>(x, qf);
+#pragma unroll
+                for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                    for (int p = QP - 1; p >= 0; p--) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kt][k], qf[p], s[kt], 0, 0, 0);
+            }
+            const bool none = st == INFINITY;
+            const bool masked = live < BLK || (int64_t)sp.y > pos0 + r0 / a.g;
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -st));
+                    acc[kt][e] += none || (masked && ids[kt][e] > pos) ? 0.f : p;
+                }
+        }
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+                float v = acc[kt][e];
+#pragma unroll
+                for (int x = 1; x < 32; x <<= 1) v += __shfl_xor(v, x);
+                if (l32 == 0) sum_l[w][kt * 32 + (e / 4) * 8 + hi * 4 + (e & 3)] = v;
+            }
+        __syncthreads();
+        if (tid < 64 && tid < live) {
+            float *wp = a.mem.weight + (size_t)si * a.cap + (size_t)J * BLK + tid;
+            *wp += (sum_l[0][tid] + sum_l[1][tid]) + (sum_l[2][tid] + sum_l[3][tid]);
+        }
+        __syncthreads();   // the sums have been read
+    }
+}
+
+}  // namespace full
+}  // namespace lola
