@@ -154,7 +154,7 @@ lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *
         else if constexpr (DH < 256) { if (a.T > 1) STEP(2, true); else STEP(2, false); }
 #undef STEP
         LAUNCH_CHECK();
-        const int jo = p.nsplit > 1 ? (R * DH + 255) / 256 : 0, jw = gather ? std::min((a.cap + 255) / 256, 4096) : 0;
+        const int jo = p.nsplit > 1 ? R : 0, jw = gather ? std::min((a.cap + 255) / 256, 4096) : 0;
         if (jo + jw) {
             hipLaunchKernelGGL((step_join_kernel<DH, TO>), dim3(S, jo + jw), dim3(256), 0, stream, sa, jo);
             LAUNCH_CHECK();
@@ -316,7 +316,10 @@ lola_status lola_full_evict(const lola_full_config *c, const lola_full_state *st
     a.edge = (float *)(ws + p.off_edge);
     a.most = p.most; a.nkb = p.nkb;
     const int S = c->batch * c->n_kv_heads;
-    hipLaunchKernelGGL(evict_select_kernel, dim3(S), dim3(1024), 0, (hipStream_t)stream, a);
+    // (up to 8192 slots in workgroups of 256, of which more fit a compute unit)
+    const int lds = a.cap <= RANKS_LDS ? a.cap * 4 : 0;
+    if (a.cap <= 8192) hipLaunchKernelGGL((evict_select_kernel<256>), dim3(S), dim3(256), lds, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL((evict_select_kernel<1024>), dim3(S), dim3(1024), lds, (hipStream_t)stream, a);
     LAUNCH_CHECK();
     if (p.nkb == 0) return LOLA_OK;
     const dim3 grid(p.nkb, S);

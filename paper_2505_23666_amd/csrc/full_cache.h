@@ -198,17 +198,17 @@ struct EvictArgs {
 };
 
 // larger rank = stays: pairs that always stay above all, then NaN, then by weight (any float, -0 = +0)
-__device__ __forceinline__ uint32_t rank_of(const EvictArgs &a, size_t at, int64_t recent_from) {
-    const int64_t i = a.mem.idx[at];
-    if (i < a.first || i >= recent_from) return 0xFFFFFFFFu;
-    const float w = a.mem.weight[at] + 0.f;
+__device__ __forceinline__ uint32_t rank_of(int i, float w, int first, int64_t recent_from) {
+    if (i < first || i >= recent_from) return 0xFFFFFFFFu;
+    w += 0.f;
     if (w != w) return 0xFFFFFFFEu;
     const uint32_t u = __float_as_uint(w);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// exclusive sum over the workgroup's 1024 threads; *total receives the sum
-__device__ __forceinline__ int scan1024(int v, int *wsum, int *total) {
+// exclusive sum over the workgroup's threads; *total receives the sum
+template <int NT>
+__device__ __forceinline__ int scan_all(int v, int *wsum, int *total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     int x = v;
 #pragma unroll
@@ -218,58 +218,110 @@ __device__ __forceinline__ int scan1024(int v, int *wsum, int *total) {
     __syncthreads();
     int base = 0, all = 0;
 #pragma unroll
-    for (int i = 0; i < 16; i++) { if (i < w) base += wsum[i]; all += wsum[i]; }
+    for (int i = 0; i < NT / 64; i++) { if (i < w) base += wsum[i]; all += wsum[i]; }
     *total = all;
     return base + x - v;
 }
 
-// One workgroup per stream: the keep-th largest rank by four passes over the ranks, eight bits each, then the lists.
-__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
-    __shared__ int hist[256], wsum[16], found[2];
+constexpr int RANKS_LDS = 32768;   // ranks that the selection keeps in LDS; longer caches compute them again in each pass
+
+// One workgroup per stream finds the keep-th largest rank in three passes over the ranks (11, 11 and 10 bits: a histogram in LDS
+// and a scan over its bins), then writes the lists.  A thread takes four slots at a time.  Bound by latency: a handful of dependent passes
+// over a few thousand ranks.
+template <int NT>
+__global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
+    constexpr int NB = 2048, BPT = NB / NT;
+    extern __shared__ __attribute__((aligned(16))) uint32_t rank_l[];     // [min(cap, RANKS_LDS)] where they fit
+    __shared__ int hist[NB], wsum[NT / 64], found[3];
     const int si = blockIdx.x, tid = threadIdx.x;
     int count = a.mem.count[si];
     count = count < 0 ? 0 : (count > a.cap ? a.cap : count);
     int32_t *before = a.before + (size_t)si * (a.nkb + 1);
     if (count <= a.keep) {
-        for (int J = tid; J <= a.nkb; J += 1024) before[J] = 0;
+        for (int J = tid; J <= a.nkb; J += NT) before[J] = 0;
         return;
     }
     const size_t base = (size_t)si * a.cap;
     const int64_t recent_from = a.mem.n_tokens[si] - a.recent;
+    const bool cached = a.cap <= RANKS_LDS;
+    // ranks of slots s .. s + 3 (s a multiple of four; beyond count: nothing looks at them)
+    auto compute = [&](int s) {
+        const int4 i = *reinterpret_cast<const int4 *>(a.mem.idx + base + s);
+        const float4 w = *reinterpret_cast<const float4 *>(a.mem.weight + base + s);
+        return make_uint4(rank_of(i.x, w.x, a.first, recent_from), rank_of(i.y, w.y, a.first, recent_from),
+                          rank_of(i.z, w.z, a.first, recent_from), rank_of(i.w, w.w, a.first, recent_from));
+    };
+    auto ranks = [&](int s) { return cached ? *reinterpret_cast<const uint4 *>(rank_l + s) : compute(s); };
     uint32_t prefix = 0, mask = 0;
-    int want = a.keep;           // of the ranks that match the prefix, the want-th largest is looked for
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+    int want = a.keep, equal = 0;       // of the ranks that match the prefix, the want-th largest is looked for
+#pragma unroll
+    for (int pass = 0; pass < 3; pass++) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t digit = pass == 2 ? 1023u : 2047u;
+        for (int i = tid; i < NB; i += NT) hist[i] = 0;
         __syncthreads();
-        for (int s = tid; s < count; s += 1024) {
-            const uint32_t u = rank_of(a, base + s, recent_from);
-            if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255u], 1);
+        for (int s = tid * 4; s < count; s += NT * 4) {
+            uint4 u;
+            if (pass == 0) {
+                u = compute(s);
+                if (cached) *reinterpret_cast<uint4 *>(rank_l + s) = u;
+            } else u = ranks(s);
+            const uint32_t us[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (s + e < count && (us[e] & mask) == prefix) atomicAdd(&hist[(us[e] >> shift) & digit], 1);
         }
         __syncthreads();
-        if (tid == 0) {
-            int left = want, v = 255;
-            while (v > 0 && hist[v] < left) left -= hist[v--];
-            found[0] = v; found[1] = left;
+        // bins from the largest down: thread t has BPT of them from NB - 1 - t BPT on
+        int mine = 0, total;
+#pragma unroll
+        for (int i = 0; i < BPT; i++) mine += hist[NB - 1 - tid * BPT - i];
+        int above = scan_all<NT>(mine, wsum, &total);
+        if (above < want && above + mine >= want) {
+            for (int i = 0; i < BPT; i++) {
+                const int v = NB - 1 - tid * BPT - i, n = hist[v];
+                if (above + n >= want) { found[0] = v; found[1] = want - above; found[2] = n; break; }
+                above += n;
+            }
         }
         __syncthreads();
-        prefix |= (uint32_t)found[0] << shift; mask |= 255u << shift; want = found[1];
+        prefix |= (uint32_t)found[0] << shift; mask |= digit << shift; want = found[1]; equal = found[2];
         __syncthreads();
     }
-    // kept: rank > prefix, and the `want` lowest slots of those with rank == prefix
+    // kept: rank > prefix, and the `want` lowest slots of the `equal` ones with rank == prefix
     int ties = 0, holes = 0, moved = 0;
-    for (int s0 = 0; s0 < count; s0 += 1024) {
-        const int s = s0 + tid;
-        const uint32_t u = s < count ? rank_of(a, base + s, recent_from) : 0u;
-        int t_all, h_all, m_all;
-        const bool tie = s < count && u == prefix;
-        const int t_at = ties + scan1024(tie, wsum, &t_all);
-        const bool kept = s < count && (u > prefix || (tie && t_at < want));
-        const bool hole = s < a.keep && !kept, mover = s >= a.keep && kept;
-        const int h_at = holes + scan1024(hole, wsum, &h_all), m_at = moved + scan1024(mover, wsum, &m_all);
-        if (s < a.keep && s % BLK == 0) before[s / BLK] = h_at;
-        if (hole) a.dst[(size_t)si * a.most + h_at] = s;
-        if (mover) a.src[(size_t)si * a.most + m_at] = s;
-        ties += t_all; holes += h_all; moved += m_all;
+    for (int s0 = 0; s0 < count; s0 += NT * 4) {
+        const int s = s0 + tid * 4;
+        const uint4 u = s < count ? ranks(s) : make_uint4(0, 0, 0, 0);
+        const uint32_t us[4] = {u.x, u.y, u.z, u.w};
+        int t_at = ties;
+        if (equal != want) {
+            int n = 0, all;
+#pragma unroll
+            for (int e = 0; e < 4; e++) n += s + e < count && us[e] == prefix;
+            t_at += scan_all<NT>(n, wsum, &all);
+            ties += all;
+        }
+        int kinds = 0, hole[4], mover[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const bool in = s + e < count, tie = in && us[e] == prefix;
+            const bool kept = in && (us[e] > prefix || (tie && t_at < want));
+            if (tie && equal != want) t_at++;
+            hole[e] = in && s + e < a.keep && !kept;
+            mover[e] = s + e >= a.keep && kept;
+            kinds += hole[e] + (mover[e] << 16);
+        }
+        int all;
+        const int at = scan_all<NT>(kinds, wsum, &all);
+        int h_at = holes + (at & 0xFFFF), m_at = moved + (at >> 16);
+        if (s % BLK == 0 && s < a.keep) before[s / BLK] = h_at;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            if (hole[e]) a.dst[(size_t)si * a.most + h_at++] = s + e;
+            if (mover[e]) a.src[(size_t)si * a.most + m_at++] = s + e;
+        }
+        holes += all & 0xFFFF; moved += all >> 16;
     }
     if (tid == 0) {
         before[a.nkb] = holes;

@@ -283,52 +283,79 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
     }
 }
 
-// Joins the shares: workgroups [0, jo) of a stream write its outputs, 256 elements each; the others, where weights are gathered, add
-// sum over rows of 2^(logit - M) / L to the weights of 256 slots at a time.
+// Joins the shares: workgroup y < jo of a stream one row of outputs (DH / 4 threads per share, the shares dealt to the groups of threads); the
+// others, where weights are gathered, add sum over rows of 2^(logit - M) / L to the weights of 256 slots at a time.
 template <int DH, typename TO>
 __global__ __launch_bounds__(256) void step_join_kernel(StepArgs sa, int jo) {
     const Args &a = sa.a;
     constexpr float SCALE = 1.f / 16384.f;           // sums hold p times 2^14
+    constexpr int TPS = DH / 4, NG = 256 / TPS;
     __shared__ float M_l[32], L_l[32];
+    __shared__ __attribute__((aligned(16))) float acc_l[NG][DH + 4];
     const int tid = threadIdx.x, si = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv, R = a.T * a.g, ns = sa.nsplit;
-    const float *ml = sa.part_ml + (size_t)si * ns * R * 2;
-    const int n = new_tokens(a, b), count = n ? held(a, si) : 0, y = blockIdx.y;
-    if (y >= jo && (y - jo) * 256 >= count) return;
-    // eight lanes per row look at the shares
-    {
-        const int r = tid >> 3, j = tid & 7;
+    const float2 *ml = reinterpret_cast<const float2 *>(sa.part_ml) + (size_t)si * ns * R;
+    const int y = blockIdx.y;
+    if (y < jo) {
+        const int gr = tid / TPS, col = (tid % TPS) * 4;
+        const int t = y / a.g, hq = h * a.g + (y - t * a.g);
+        const float *po = sa.part_o + ((size_t)si * ns * R + y) * DH + col;
+        // every group of threads a running maximum and sum over its shares (an empty share: maximum -inf, sum 0, outputs 0)
         float M = -INFINITY, L = 0.f;
-        if (r < R) {
-            for (int s = j; s < ns; s += 8) M = fmaxf(M, ml[(s * R + r) * 2]);
-            M = fmaxf(M, __shfl_xor(M, 1)); M = fmaxf(M, __shfl_xor(M, 2)); M = fmaxf(M, __shfl_xor(M, 4));
-            const float mu = M == -INFINITY ? 0.f : M;
-            for (int s = j; s < ns; s += 8) L += ml[(s * R + r) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(s * R + r) * 2] - mu);
-            L += __shfl_xor(L, 1); L += __shfl_xor(L, 2); L += __shfl_xor(L, 4);
-            if (j == 0) { M_l[r] = mu; L_l[r] = L; }
+        f4 acc = (f4){0.f, 0.f, 0.f, 0.f};
+        for (int s0 = gr; s0 < ns; s0 += 4 * NG) {
+            float2 p[4];
+            f4 o[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int s = s0 + i * NG;
+                p[i] = s < ns ? ml[s * R + y] : make_float2(-INFINITY, 0.f);
+                o[i] = s < ns ? *reinterpret_cast<const f4 *>(po + (size_t)s * R * DH) : (f4){0.f, 0.f, 0.f, 0.f};
+            }
+            const float mn = fmaxf(fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x)), M), mu = mn == -INFINITY ? 0.f : mn;
+            const float f = __builtin_amdgcn_exp2f(M - mu);
+            M = mn; L *= f; acc *= f;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const float x = p[i].y * __builtin_amdgcn_exp2f(p[i].x - mu);
+                L += x; acc += o[i] * x;
+            }
         }
+        *reinterpret_cast<f4 *>(&acc_l[gr][col]) = acc;
+        if (tid % TPS == 0) { M_l[gr] = M; L_l[gr] = L; }
+        __syncthreads();
+        if (tid < DH) {
+            float Mx = -INFINITY, Ls = 0.f, v = 0.f;
+            for (int i = 0; i < NG; i++) Mx = fmaxf(Mx, M_l[i]);
+            const float mu = Mx == -INFINITY ? 0.f : Mx;
+            for (int i = 0; i < NG; i++) {
+                const float f = __builtin_amdgcn_exp2f(M_l[i] - mu);
+                Ls += L_l[i] * f; v += acc_l[i][tid] * f;
+            }
+            stf((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st, tid, Ls == 0.f ? 0.f : v / Ls);
+        }
+        return;
+    }
+    const int n = new_tokens(a, b), count = n ? held(a, si) : 0;
+    if ((y - jo) * 256 >= count) return;
+    // eight lanes per row look at the shares
+    const int r8 = tid >> 3, j = tid & 7;
+    if (r8 < R) {
+        float M = -INFINITY, L = 0.f;
+        for (int s = j; s < ns; s += 8) M = fmaxf(M, ml[s * R + r8].x);
+        M = fmaxf(M, __shfl_xor(M, 1)); M = fmaxf(M, __shfl_xor(M, 2)); M = fmaxf(M, __shfl_xor(M, 4));
+        const float mu = M == -INFINITY ? 0.f : M;
+        for (int s = j; s < ns; s += 8) { const float2 p = ml[s * R + r8]; L += p.y * __builtin_amdgcn_exp2f(p.x - mu); }
+        L += __shfl_xor(L, 1); L += __shfl_xor(L, 2); L += __shfl_xor(L, 4);
+        if (j == 0) { M_l[r8] = mu; L_l[r8] = L > 0.f && finite(L) ? 1.f / (L * SCALE) : 0.f; }
     }
     __syncthreads();
-    if (y < jo) {
-        const int e = y * 256 + tid;
-        if (e >= R * DH) return;
-        const int r = e / DH, col = e - r * DH, t = r / a.g, hq = h * a.g + (r - t * a.g);
-        const float mu = M_l[r], L = L_l[r];
+    for (int slot = (y - jo) * 256 + tid; slot < count; slot += (gridDim.y - jo) * 256) {
         float acc = 0.f;
-        for (int s = 0; s < ns; s++) {
-            const float ms = ml[(s * R + r) * 2], ls = ml[(s * R + r) * 2 + 1];
-            // (an empty share's maximum is -inf: weight 0; its outputs are zeros)
-            acc += sa.part_o[(((size_t)si * ns + s) * R + r) * DH + col] * (ls * __builtin_amdgcn_exp2f(ms - mu));
+        for (int r = 0; r < n * a.g; r++) {
+            const float f = L_l[r];
+            if (f != 0.f) acc += __builtin_amdgcn_exp2f(sa.logit[((size_t)si * R + r) * a.cap + slot] - M_l[r]) * f;
         }
-        stf((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st, col, L == 0.f ? 0.f : acc / L);
-    } else {
-        for (int slot = (y - jo) * 256 + tid; slot < count; slot += (gridDim.y - jo) * 256) {
-            float acc = 0.f;
-            for (int r = 0; r < n * a.g; r++) {
-                const float L = L_l[r];
-                if (L > 0.f && finite(L)) acc += __builtin_amdgcn_exp2f(sa.logit[((size_t)si * R + r) * a.cap + slot] - M_l[r]) / (L * SCALE);
-            }
-            a.mem.weight[(size_t)si * a.cap + slot] += acc;
-        }
+        a.mem.weight[(size_t)si * a.cap + slot] += acc;
     }
 }
 
