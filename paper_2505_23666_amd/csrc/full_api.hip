@@ -68,7 +68,7 @@ constexpr int PROMPT_NW = 4;       // wavefronts (of 32 rows) per workgroup of t
 struct AttendPlan {
     bool step;
     int nsplit, ntiles;
-    size_t off_stat, off_o, off_ml, off_logit, off_span, bytes;
+    size_t off_stat, off_o, off_ml, off_logit, off_counts, off_span, bytes;
 };
 AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
     const size_t S = (size_t)c->batch * c->n_kv_heads, R = (size_t)T * (c->n_q_heads / c->n_kv_heads);
@@ -82,6 +82,7 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
         p.off_o = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * c->head_dim * 4);
         p.off_ml = off; if (p.nsplit > 1 || gather) off += up(S * p.nsplit * R * 2 * 4);
         p.off_logit = off; if (gather) off += up(S * R * c->capacity * 4);
+        p.off_counts = off; if (gather) off += up(S * 4);
     } else {
         p.ntiles = (int)((R + 32 * PROMPT_NW - 1) / (32 * PROMPT_NW));
         // two workgroups fit a compute unit; fewer are split over the blocks, four blocks each at least when the cache is full
@@ -141,17 +142,20 @@ lola_status run_append(const Args &a, hipStream_t stream) {
 
 template <int DH, typename TI, typename TO>
 lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *ws, hipStream_t stream) {
+    const bool fused = a.k != nullptr;     // a generation step whose token the step kernel puts into the cache
     if (p.step) {
         StepArgs sa;
         sa.a = a; sa.nsplit = p.nsplit;
         sa.part_o = p.nsplit > 1 ? (float *)(ws + p.off_o) : nullptr;
         sa.part_ml = p.nsplit > 1 || gather ? (float *)(ws + p.off_ml) : nullptr;
         sa.logit = gather ? (float *)(ws + p.off_logit) : nullptr;
+        sa.append = fused && sa.part_ml;
+        sa.counts = fused && gather ? (int32_t *)(ws + p.off_counts) : nullptr;
         const int S = a.B * a.Hkv, R = a.T * a.g;
         const dim3 grid(S, p.nsplit);
-#define STEP(CT, M) hipLaunchKernelGGL((step_kernel<DH, CT, TI, TO, M>), grid, dim3(256), 0, stream, sa)
-        if (R <= 16) { if (a.T > 1) STEP(1, true); else STEP(1, false); }
-        else if constexpr (DH < 256) { if (a.T > 1) STEP(2, true); else STEP(2, false); }
+#define STEP(CT, M, AP) hipLaunchKernelGGL((step_kernel<DH, CT, TI, TO, M, AP>), grid, dim3(256), 0, stream, sa)
+        if (R <= 16) { if (fused) STEP(1, false, true); else if (a.T > 1) STEP(1, true, false); else STEP(1, false, false); }
+        else if constexpr (DH < 256) { if (fused) STEP(2, false, true); else if (a.T > 1) STEP(2, true, false); else STEP(2, false, false); }
 #undef STEP
         LAUNCH_CHECK();
         const int jo = p.nsplit > 1 ? R : 0, jw = gather ? std::min((a.cap + 255) / 256, 4096) : 0;
@@ -197,10 +201,11 @@ lola_status run_attend(const Args &a, const AttendPlan &p, int gather, char *ws,
     }
 }
 
-lola_status attend(const lola_full_config *c, const lola_full_state *st, const void *q, const int32_t *lens, int32_t T, int32_t gather,
-                   void *out, void *workspace, hipStream_t stream) {
+// k, v: NULL, or a token per sequence that the step kernel puts into the cache first (plans with p.step, T = 1)
+lola_status attend(const lola_full_config *c, const lola_full_state *st, const void *q, const void *k, const void *v, const int32_t *lens,
+                   int32_t T, int32_t gather, void *out, void *workspace, hipStream_t stream) {
     Args a = make_args(c, st, T, lens);
-    a.q = q; a.out = out;
+    a.q = q; a.k = k; a.v = v; a.out = out;
     const AttendPlan p = plan_attend(c, T, gather);
     char *ws = (char *)workspace;
     const bool bo = c->out_dtype == LOLA_BF16;
@@ -277,7 +282,7 @@ lola_status lola_full_attend(const lola_full_config *c, const lola_full_state *s
     rc = check_attend(c, st, q, T, gather, out, workspace, workspace_bytes);
     if (rc != LOLA_OK) return rc;
     if (lens && misaligned(lens)) return LOLA_ERR_ALIGN;
-    return attend(c, st, q, lens, T, gather, out, workspace, (hipStream_t)stream);
+    return attend(c, st, q, nullptr, nullptr, lens, T, gather, out, workspace, (hipStream_t)stream);
 }
 
 lola_status lola_full_step(const lola_full_config *c, const lola_full_state *st, const void *q, const void *k, const void *v,
@@ -291,9 +296,10 @@ lola_status lola_full_step(const lola_full_config *c, const lola_full_state *st,
     rc = check_attend(c, st, q, 1, gather, out, workspace, workspace_bytes);
     if (rc != LOLA_OK) return rc;
     if (misaligned(k) || misaligned(v)) return LOLA_ERR_ALIGN;
-    rc = append(c, st, k, v, nullptr, 1, (hipStream_t)stream);
+    if (plan_attend(c, 1, gather).step) return attend(c, st, q, k, v, nullptr, 1, gather, out, workspace, (hipStream_t)stream);
+    rc = append(c, st, k, v, nullptr, 1, (hipStream_t)stream);      // more query heads per kv head than the step kernel takes
     if (rc != LOLA_OK) return rc;
-    return attend(c, st, q, nullptr, 1, gather, out, workspace, (hipStream_t)stream);
+    return attend(c, st, q, nullptr, nullptr, nullptr, 1, gather, out, workspace, (hipStream_t)stream);
 }
 
 lola_status lola_full_evict(const lola_full_config *c, const lola_full_state *st, int32_t keep, int32_t first, int32_t recent,

@@ -70,6 +70,8 @@ struct StepArgs {
     float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
     float *part_ml;    // [S][nsplit][R][2] running maximum (powers of two) and sum; sum 0: an empty share
     float *logit;      // [S][R][cap] logits (powers of two) where weights are gathered, else NULL
+    int32_t *counts;   // [S] with a token appended by the same launch and weights gathered: the slots in use after it
+    int append;        // the join moves the counters on (a.k, a.v hold the token)
 };
 
 // swizzle of the 16-byte pieces of an LDS row of DH bytes: rows whose addresses differ by a multiple of 256 bytes meet other banks
@@ -79,7 +81,59 @@ __device__ __forceinline__ int vswz(int row) { return (row / (256 / DH)) & (DH /
 __device__ __forceinline__ float quad_max(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
 __device__ __forceinline__ float quad_sum(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 
-template <int DH, int CT, typename TI, typename TO, bool MASK>
+// Puts the stream's new token into slot c0, by one wavefront: lanes below DH / 8 take eight elements of the key each, as many behind them the value.
+// The same codes, scales and rules as append_kernel.
+template <int DH, typename TI>
+__device__ __forceinline__ void append_token(const Args &a, int si, int b, int h, int c0, int lane) {
+    constexpr int NL = DH / 8;
+    const int J = c0 / BLK, off = c0 % BLK, part = lane % NL;
+    const bool isk = lane < NL, mine = lane < 2 * NL;
+    const int64_t told = a.mem.n_tokens[si];
+    float *kss = a.mem.ks + (size_t)si * a.nblk + J, *vss = a.mem.vs + (size_t)si * a.nblk + J;
+    const float oks = *kss, ovs = *vss;      // (of a block that held nothing: not looked at)
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = 0.f;
+    if (mine) load8((const TI *)(isk ? a.k : a.v) + b * a.k_sb + h * a.k_sh + part * 8, x);
+    float top = 0.f;
+    bool nf = false;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        if (!finite(x[e])) { nf = true; x[e] = 0.f; }
+        top = fmaxf(top, fabsf(x[e]));
+    }
+    const bool bad = __any(nf);
+    const float ak = bad ? 0.f : wave_max(isk ? top : 0.f), av = wave_max(isk ? 0.f : top);
+    int ek = fit_exponent(ak), ev = fit_exponent(av);
+    uint8_t *kb = a.mem.k + ((size_t)si * a.cap + (size_t)J * BLK) * DH, *vb = a.mem.v + ((size_t)si * a.cap + (size_t)J * BLK) * DH;
+    if (off > 0) {
+        const int ok = exponent_of(oks), ov = exponent_of(ovs);
+        ek = max(ek, ok); ev = max(ev, ov);
+        if (ek > ok || ev > ov) {
+            const float fk = pow2(max(ok - ek, -40)), fv = pow2(max(ov - ev, -40));
+            for (int e = lane; e < off * NL; e += 64) {
+                if (ek > ok) { uint2 u = reinterpret_cast<uint2 *>(kb)[e]; u.x = rescale_codes(u.x, fk); u.y = rescale_codes(u.y, fk); reinterpret_cast<uint2 *>(kb)[e] = u; }
+                if (ev > ov) { uint2 u = reinterpret_cast<uint2 *>(vb)[e]; u.x = rescale_codes(u.x, fv); u.y = rescale_codes(u.y, fv); reinterpret_cast<uint2 *>(vb)[e] = u; }
+            }
+        }
+    }
+    if (mine) {
+        const float f = pow2(isk ? -ek : -ev);
+        uint2 u;
+        u.x = to_codes(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+        u.y = to_codes(x[4] * f, x[5] * f, x[6] * f, x[7] * f);
+        if (isk && bad) u.x = u.y = 0x7F7F7F7Fu;
+        *reinterpret_cast<uint2 *>((isk ? kb : vb) + off * DH + part * 8) = u;
+    }
+    if (lane == 0) {
+        *kss = pow2(ek); *vss = pow2(ev);
+        a.mem.idx[(size_t)si * a.cap + c0] = (int32_t)told;
+        if (a.mem.weight) a.mem.weight[(size_t)si * a.cap + c0] = 0.f;
+    }
+    __threadfence_block();      // this wavefront reads the block back
+}
+
+template <int DH, int CT, typename TI, typename TO, bool MASK, bool APPEND>
 __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
     constexpr int QP = sizeof(TI) == 4 ? 3 : 1, PP = sizeof(TO) == 4 ? 2 : 1;
     constexpr int NK = DH / 32;                     // contraction steps of the first product
@@ -92,9 +146,11 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
     const Args &a = sa.a;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
     const int si = blockIdx.x, split = blockIdx.y, b = si / a.Hkv, h = si - b * a.Hkv;
-    const int R = a.T * a.g, n = new_tokens(a, b), count = n ? held(a, si) : 0;
+    const int R = a.T * a.g, n = new_tokens(a, b), c0 = n ? held(a, si) : 0, count = APPEND ? min(c0 + 1, a.cap) : c0;
     const int nb = (count + BLK - 1) / BLK;
     const int J0 = (int)((int64_t)nb * split / sa.nsplit), J1 = (int)((int64_t)nb * (split + 1) / sa.nsplit);
+    // a step's own token goes into the stream's last block, by the wavefront that reads it (nobody else does)
+    if (APPEND && count > c0 && J1 == nb && J1 > J0 && (nb - 1 - J0) % STEP_NW == w) append_token<DH, TI>(a, si, b, h, c0, lane);
     const uint8_t *kc = a.mem.k + (size_t)si * a.cap * DH, *vc = a.mem.v + (size_t)si * a.cap * DH;
     const float *ks = a.mem.ks + (size_t)si * a.nblk, *vs = a.mem.vs + (size_t)si * a.nblk;
     const int32_t *idx = a.mem.idx + (size_t)si * a.cap;
@@ -244,6 +300,10 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
 #pragma unroll
         for (int ct = 0; ct < CT; ct++) { ml_l[w][0][ct * 16 + n16] = m[ct]; ml_l[w][1][ct * 16 + n16] = l[ct]; }
     __syncthreads();
+    if (APPEND && tid == 0) {
+        if (!sa.part_ml) { a.mem.count[si] = count; a.mem.n_tokens[si] += 1; }       // (the stream's only workgroup)
+        else if (sa.counts && split == 0) sa.counts[si] = count;
+    }
 #pragma unroll
     for (int ct = 0; ct < CT; ct++) {
         float *ol = reinterpret_cast<float *>(stage[0]);     // [wavefront][column][16 rows]
@@ -295,6 +355,10 @@ __global__ __launch_bounds__(256) void step_join_kernel(StepArgs sa, int jo) {
     const int tid = threadIdx.x, si = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv, R = a.T * a.g, ns = sa.nsplit;
     const float2 *ml = reinterpret_cast<const float2 *>(sa.part_ml) + (size_t)si * ns * R;
     const int y = blockIdx.y;
+    if (sa.append && y == 0 && tid == 0) {    // (nobody else of this launch looks at them)
+        a.mem.count[si] = min(held(a, si) + 1, a.cap);
+        a.mem.n_tokens[si] += 1;
+    }
     if (y < jo) {
         const int gr = tid / TPS, col = (tid % TPS) * 4;
         const int t = y / a.g, hq = h * a.g + (y - t * a.g);
@@ -335,7 +399,7 @@ __global__ __launch_bounds__(256) void step_join_kernel(StepArgs sa, int jo) {
         }
         return;
     }
-    const int n = new_tokens(a, b), count = n ? held(a, si) : 0;
+    const int n = new_tokens(a, b), count = sa.append ? sa.counts[si] : n ? held(a, si) : 0;
     if ((y - jo) * 256 >= count) return;
     // eight lanes per row look at the shares
     const int r8 = tid >> 3, j = tid & 7;
