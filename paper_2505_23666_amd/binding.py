@@ -117,7 +117,8 @@ def _ptr(t):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """Handle of the current device's current stream (without the stream object that torch.cuda.current_stream() makes: 0.3 us, not 2.6)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def lola_state_bytes(cfg: LolaConfig):
@@ -178,8 +179,8 @@ def lola_full_workspace_bytes(cfg: LolaFullConfig, T: int, gather: bool = False)
     return int(lib().lola_full_workspace_bytes(C.byref(cfg), int(T), int(gather)))
 
 
-def _sized(t):
-    return _ptr(t), 0 if t is None else t.numel() * t.element_size()
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def lola_full_init(cfg: LolaFullConfig, st: LolaFullState) -> None:
@@ -187,22 +188,22 @@ def lola_full_init(cfg: LolaFullConfig, st: LolaFullState) -> None:
 
 
 def lola_full_append(cfg, st, k, v, lens, T) -> None:
-    _check(lib().lola_full_append(C.byref(cfg), C.byref(st), _ptr(k), _ptr(v), _ptr(lens), int(T), _stream()), "lola_full_append")
+    _check(lib().lola_full_append(C.byref(cfg), C.byref(st), _addr(k), _addr(v), _addr(lens), T, _stream()), "lola_full_append")
 
 
 def lola_full_attend(cfg, st, q, lens, T, gather, out, workspace) -> None:
-    _check(lib().lola_full_attend(C.byref(cfg), C.byref(st), _ptr(q), _ptr(lens), int(T), int(gather), _ptr(out), *_sized(workspace),
-                                  _stream()), "lola_full_attend")
+    _check(lib().lola_full_attend(C.byref(cfg), C.byref(st), _addr(q), _addr(lens), T, gather, _addr(out), _addr(workspace),
+                                  0 if workspace is None else workspace.nbytes, _stream()), "lola_full_attend")
 
 
 def lola_full_step(cfg, st, q, k, v, gather, out, workspace) -> None:
-    _check(lib().lola_full_step(C.byref(cfg), C.byref(st), _ptr(q), _ptr(k), _ptr(v), int(gather), _ptr(out), *_sized(workspace),
-                                _stream()), "lola_full_step")
+    _check(lib().lola_full_step(C.byref(cfg), C.byref(st), _addr(q), _addr(k), _addr(v), gather, _addr(out), _addr(workspace),
+                                0 if workspace is None else workspace.nbytes, _stream()), "lola_full_step")
 
 
 def lola_full_evict(cfg, st, keep, first, recent, workspace) -> None:
-    _check(lib().lola_full_evict(C.byref(cfg), C.byref(st), int(keep), int(first), int(recent), *_sized(workspace), _stream()),
-           "lola_full_evict")
+    _check(lib().lola_full_evict(C.byref(cfg), C.byref(st), keep, first, recent, _addr(workspace),
+                                 0 if workspace is None else workspace.nbytes, _stream()), "lola_full_evict")
 
 
 _TORCH_DT = {LOLA_F32: torch.float32, LOLA_BF16: torch.bfloat16}
@@ -320,6 +321,8 @@ class LolaFullCache:
     def __init__(self, B, Hq, Hkv, d, capacity, dtype="bf16", out_dtype="f32", scale=0.0, tokens_first=False, weights=True,
                  buffers=None, device="cuda:0"):
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
         cap = -(-int(capacity) // LOLA_FULL_BLOCK) * LOLA_FULL_BLOCK
         self.dt = LOLA_BF16 if dtype == "bf16" else LOLA_F32
         self.odt = LOLA_BF16 if out_dtype == "bf16" else LOLA_F32
@@ -348,14 +351,20 @@ class LolaFullCache:
         self.st = LolaFullState(*[None if t is None else t.data_ptr() for t in fields])
         self.workspace = None
         self._ws_bytes = {}
+        self._q1, self._k1 = (B, Hq, d), (B, Hkv, d)
         self.fill = 0 if buffers is None else cap   # at least as many slots as any stream has in use
         if buffers is None:
             self.reset()
 
+    def _on_device(self, f, *args):
+        if torch.cuda.current_device() == self.device.index:
+            return f(*args)
+        with torch.cuda.device(self.device):
+            return f(*args)
+
     def reset(self):
         """Empty caches."""
-        with torch.cuda.device(self.device):
-            lola_full_init(self.cfg, self.st)
+        self._on_device(lola_full_init, self.cfg, self.st)
         self.fill = 0
 
     def _ws(self, T, gather):
@@ -400,35 +409,41 @@ class LolaFullCache:
         T = self._tokens(k, self.Hkv)
         self._tokens(v, self.Hkv, T)
         self._lens(lens)
-        with torch.cuda.device(self.device):
-            self._room(T, lens)
-            lola_full_append(self.cfg, self.st, k, v, lens, T)
+        self._on_device(self._append, k, v, lens, T)
+
+    def _append(self, k, v, lens, T):
+        self._room(T, lens)
+        lola_full_append(self.cfg, self.st, k, v, lens, T)
 
     def attend(self, q, lens=None, out=None, gather=False):
         """Outputs of the newest tokens' queries q [B, Hq, T, d] ([B, T, Hq, d]); gather adds their weights to `weight`."""
         T = self._tokens(q, self.Hq)
         self._lens(lens)
         out = self._out(out, q.shape)
-        with torch.cuda.device(self.device):
-            lola_full_attend(self.cfg, self.st, q, lens, T, gather, out, self._ws(T, bool(gather)))
+        gather = 1 if gather else 0
+        self._on_device(lola_full_attend, self.cfg, self.st, q, lens, T, gather, out, self._ws(T, gather))
         return out
 
     def step(self, q, k, v, out=None, gather=False):
         """append and attend of one token per sequence: q [B, Hq, d], k, v [B, Hkv, d]."""
-        want, dt = (self.B, self.Hkv, self.d), _TORCH_DT[self.dt]
-        if q.shape != (self.B, self.Hq, self.d) or k.shape != want or v.shape != want:
-            raise LolaError(f"q {(self.B, self.Hq, self.d)}, k and v {want} expected")
+        if q.shape != self._q1 or k.shape != self._k1 or v.shape != self._k1:
+            raise LolaError(f"q {self._q1}, k and v {self._k1} expected")
+        dt, dev = _TORCH_DT[self.dt], self.device
         for x in (q, k, v):
-            if x.dtype != dt or x.device != self.device or not x.is_contiguous():
-                raise LolaError(f"contiguous {dt} on {self.device} expected")
-        out = self._out(out, q.shape)
-        with torch.cuda.device(self.device):
-            self._room(1, None)
-            lola_full_step(self.cfg, self.st, q, k, v, gather, out, self._ws(1, bool(gather)))
+            if x.dtype != dt or x.device != dev or not x.is_contiguous():
+                raise LolaError(f"contiguous {dt} on {dev} expected")
+        out = self._out(out, self._q1)
+        self._on_device(self._step, q, k, v, out, 1 if gather else 0)
         return out
+
+    def _step(self, q, k, v, out, gather):
+        if self.fill < self.capacity:
+            self.fill += 1
+        else:
+            self._room(1, None)
+        lola_full_step(self.cfg, self.st, q, k, v, gather, out, self._ws(1, gather))
 
     def evict(self, keep, first=0, recent=0):
         """Cut every stream to `keep` pairs: the first `first` and the most recent `recent` tokens, then those of largest weight."""
-        with torch.cuda.device(self.device):
-            lola_full_evict(self.cfg, self.st, keep, first, recent, self._ws(0, False))
+        self._on_device(lola_full_evict, self.cfg, self.st, int(keep), int(first), int(recent), self._ws(0, 0))
         self.fill = min(self.fill, keep)

@@ -66,7 +66,7 @@ inline size_t step_rows(int head_dim) { return head_dim == 256 ? 16 : 32; }
 constexpr int PROMPT_NW = 4;       // wavefronts (of 32 rows) per workgroup of the prompt kernel
 
 struct AttendPlan {
-    bool step;
+    bool step, wide;    // wide: one workgroup of eight wavefronts has all of a stream
     int nsplit, ntiles;
     size_t off_stat, off_o, off_ml, off_logit, off_counts, off_span, bytes;
 };
@@ -76,9 +76,15 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
     p.step = R <= step_rows(c->head_dim);
     size_t off = 0;
     if (p.step) {
-        // four workgroups per compute unit; each wavefront of one has a block at least when the cache is full
-        const size_t most = ((size_t)c->capacity / BLK + STEP_NW - 1) / STEP_NW;
-        p.nsplit = (int)std::max((size_t)1, std::min(most, (4 * CHIP_CUS + S - 1) / S));
+        // Four workgroups per compute unit, and shares of at most 8192 slots (sequences of unequal lengths); each wavefront has a
+        // block at least when the cache is full.
+        const size_t most = ((size_t)c->capacity / BLK + 3) / 4;
+        p.nsplit = (int)std::max((size_t)1, std::min(most, std::max((4 * CHIP_CUS + S - 1) / S, (size_t)c->capacity / 8192)));
+        // One workgroup of eight wavefronts per stream, and no join, where the streams fill the chip (256 streams of 4096 pairs at
+        // d = 128 46 us a step, 50 in four shares each; 512 streams 105 and 108; but 128 streams of up to 8192 pairs 80 and 66) or the cache is
+        // short (8 streams of 512 slots at d = 64 5.7 us, joined 7.0; but 1024 slots 7.1 and 6.8).
+        p.wide = R <= 16 && c->head_dim < 256 && (c->capacity <= 512 || (S >= CHIP_CUS && c->capacity <= 8192));
+        if (p.wide) p.nsplit = 1;
         p.off_o = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * c->head_dim * 4);
         p.off_ml = off; if (p.nsplit > 1 || gather) off += up(S * p.nsplit * R * 2 * 4);
         p.off_logit = off; if (gather) off += up(S * R * c->capacity * 4);
@@ -153,9 +159,14 @@ lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *
         sa.counts = fused && gather ? (int32_t *)(ws + p.off_counts) : nullptr;
         const int S = a.B * a.Hkv, R = a.T * a.g;
         const dim3 grid(S, p.nsplit);
-#define STEP(CT, M, AP) hipLaunchKernelGGL((step_kernel<DH, CT, TI, TO, M, AP>), grid, dim3(256), 0, stream, sa)
-        if (R <= 16) { if (fused) STEP(1, false, true); else if (a.T > 1) STEP(1, true, false); else STEP(1, false, false); }
-        else if constexpr (DH < 256) { if (fused) STEP(2, false, true); else if (a.T > 1) STEP(2, true, false); else STEP(2, false, false); }
+#define STEP(CT, NW, M, AP) hipLaunchKernelGGL((step_kernel<DH, CT, NW, TI, TO, M, AP>), grid, dim3(64 * NW), 0, stream, sa)
+#define STEP3(CT, NW) if (fused) STEP(CT, NW, false, true); else if (a.T > 1) STEP(CT, NW, true, false); else STEP(CT, NW, false, false)
+        if constexpr (DH < 256) {
+            if (p.wide) { STEP3(1, 8); }
+            else if (R <= 16) { STEP3(1, 4); }
+            else { STEP3(2, 4); }
+        } else { STEP3(1, 4); }
+#undef STEP3
 #undef STEP
         LAUNCH_CHECK();
         const int jo = p.nsplit > 1 ? R : 0, jw = gather ? std::min((a.cap + 255) / 256, 4096) : 0;
@@ -172,7 +183,7 @@ lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *
     pa.part_ml = p.nsplit > 1 ? (float *)(ws + p.off_ml) : nullptr;
     pa.stat = gather ? (float *)(ws + p.off_stat) : nullptr;
     const int S = a.B * a.Hkv, R = a.T * a.g;
-    constexpr int LDS = 4 * BLK * DH * 2;
+    constexpr int LDS = 4 * BLK * DH * 2 + 2 * BLK * 4;
     hipLaunchKernelGGL(span_kernel, dim3(std::min((a.nblk + 3) / 4, 256), S), dim3(256), 0, stream, pa);
     LAUNCH_CHECK();
     hipLaunchKernelGGL((prompt_kernel<DH, PROMPT_NW, TI, TO>), dim3((unsigned)S * p.ntiles * p.nsplit), dim3(64 * PROMPT_NW), LDS, stream, pa);

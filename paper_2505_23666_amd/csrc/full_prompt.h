@@ -52,8 +52,15 @@ __device__ __forceinline__ h4 lds_read_tr16(const _Float16 *p) {
 template <int DH> __device__ __forceinline__ int kswz2(int row) { return DH >= 128 ? row & 15 : DH == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 template <int DH> __device__ __forceinline__ int vswz2(int row) { return DH >= 128 ? (row & 3) << 2 : DH == 64 ? (row & 2) << 1 : 0; }
 
-__device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
-__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32); }
+// four values to consecutive elements of an output row
+__device__ __forceinline__ void store4(float *p, f4 v) { *reinterpret_cast<f4 *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, f4 v) {
+    typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+    b4 u;
+#pragma unroll
+    for (int e = 0; e < 4; e++) u[e] = (__bf16)v[e];
+    *reinterpret_cast<b4 *>(p) = u;
+}
 
 template <int DH, int NW, typename TI, typename TO>
 __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void prompt_kernel(PromptArgs pa) {
@@ -62,8 +69,8 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     constexpr int NTHR = 64 * NW, TPR = DH / 16;        // threads per row of codes (16 each)
     constexpr int NL = BLK * TPR / NTHR < 1 ? 1 : BLK * TPR / NTHR;   // 16-byte loads per thread
     constexpr bool ALL = BLK * TPR >= NTHR;             // every thread loads
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two buffers of keys [64][DH] bf16 and values [64][DH] fp16
-    constexpr int HALF = BLK * DH * 2, BUF = 2 * HALF;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two buffers of keys [64][DH] bf16, values [64][DH] fp16, indices [64]
+    constexpr int HALF = BLK * DH * 2, BUF = 2 * HALF + BLK * 4;      // (and the pairs' token indices)
     const Args &a = pa.a;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const int S = a.B * a.Hkv;
@@ -82,16 +89,36 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     const int2 *span = pa.span + (size_t)si * a.nblk;
     const int nb = (count + BLK - 1) / BLK;
     const int J0 = (int)((int64_t)nb * split / pa.nsplit), J1 = (int)((int64_t)nb * (split + 1) / pa.nsplit);
-    auto next = [&](int J) { while (J < J1 && (int64_t)span[J].x > wg_last) J++; return J; };
+    // What is known of 64 blocks from `base` on, one per lane, and which of them any query of the workgroup sees.  (Read block by
+    // block they would be scalar loads, which every wait for LDS then waits for too.)
+    int base = J0;
+    int2 spT;
+    float ksT, vsT;
+    uint64_t seen;
+    auto table = [&](int J) {
+        base = J;
+        const int x = min(J + lane, a.nblk - 1);
+        spT = span[x]; ksT = ks[x]; vsT = vs[x];
+        seen = __ballot(J + lane < J1 && (int64_t)spT.x <= wg_last);
+    };
+    auto lane_of = [&](int v, int J) { return __builtin_amdgcn_readlane(v, J - base); };
+    auto lane_of_f = [&](float v, int J) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), J - base)); };
+    // the next block from J on that is seen; the table holds it afterwards
+    auto next = [&](int J) {
+        while (true) {
+            if (J >= J1) return J1;
+            if (J >= base + 64) table(J);
+            const uint64_t rest = seen >> (J - base);
+            if (rest) return J + __builtin_ctzll(rest);
+            J = base + 64;
+        }
+    };
 
     bf8 qf[NK][QP];
 #pragma unroll
     for (int s = 0; s < NK; s++) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = 0.f;
-        if (t < n) load8((const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st + s * 16 + hi * 8, x);
-        split_bf16<QP>(x, qf[s]);
+        if (t < n) load_query((const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st + s * 16 + hi * 8, qf[s]);
+        else zero_query<QP>(qf[s]);
     }
     f16v o[ND];
 #pragma unroll
@@ -101,7 +128,9 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     float m = -INFINITY, l = 0.f;          // (l: this lane's half of the row)
 
     uint4 kr[NL], vr[NL];
+    int idr = 0;
     auto load = [&](int J) {
+        if (tid < BLK) idr = idx[(size_t)J * BLK + tid];
         const uint8_t *kp = kc + (size_t)J * BLK * DH, *vp = vc + (size_t)J * BLK * DH;
 #pragma unroll
         for (int i = 0; i < NL; i++)
@@ -112,6 +141,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     };
     auto store = [&](uint8_t *buf, int J, float vscale) {
         const int live = count - J * BLK;
+        if (tid < BLK) reinterpret_cast<int *>(buf + 2 * HALF)[tid] = tid < live ? idr : 0x7FFFFFFF;    // (no pair: later than all queries)
 #pragma unroll
         for (int i = 0; i < NL; i++)
             if (ALL || tid < BLK * TPR) {
@@ -125,18 +155,20 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             }
     };
 
-    int J = next(J0), cur = 0;
-    float vref = 0.f, vstage = 0.f;      // o is in units of vref; the staged block's values in units of vstage
+    int cur = 0, J = J1;
+    if (J0 < J1) { table(J0); J = next(J0); }
+    float vref = 0.f, vstage = 0.f, c = 0.f;      // o is in units of vref; the staged block's values in units of vstage
+    bool masked = false;
     if (J < J1) {
         load(J);
-        vstage = vs[J];
+        vstage = lane_of_f(vsT, J);
+        c = lane_of_f(ksT, J) * a.scale2;
+        masked = (int64_t)lane_of(spT.y, J) > w_first;
         store(lds, J, 1.f);
     }
     lds_barrier();
     while (J < J1) {
         const int Jn = next(J + 1);
-        const float c = ks[J] * a.scale2;
-        const bool masked = (int64_t)span[J].y > w_first;
         if (Jn < J1) load(Jn);
         const uint8_t *kb = lds + cur * BUF;
         const _Float16 *vb = reinterpret_cast<const _Float16 *>(kb + HALF);
@@ -154,17 +186,16 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             }
         }
         if (masked) {
-            const int live = count - J * BLK;
+            const int *ids_l = reinterpret_cast<const int *>(kb + 2 * HALF);
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
-                    const int at = kt * 32 + q * 8 + hi * 4;
-                    const int4 id = *reinterpret_cast<const int4 *>(idx + (size_t)J * BLK + at);
+                    const int4 id = *reinterpret_cast<const int4 *>(ids_l + kt * 32 + q * 8 + hi * 4);
                     const int ids[4] = {id.x, id.y, id.z, id.w};
 #pragma unroll
                     for (int e = 0; e < 4; e++)
-                        if (at + e >= live || ids[e] > pos) s[kt][q * 4 + e] = -INFINITY;
+                        if (ids[e] > pos) s[kt][q * 4 + e] = -INFINITY;
                 }
         }
         float mb = -INFINITY;
@@ -218,8 +249,10 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             }
         }
         if (Jn < J1) {
-            const float v = vs[Jn];
+            const float v = lane_of_f(vsT, Jn);
             vstage = fmaxf(vstage, v);
+            c = lane_of_f(ksT, Jn) * a.scale2;
+            masked = (int64_t)lane_of(spT.y, Jn) > w_first;
             store(lds + (cur ^ 1) * BUF, Jn, v / vstage);
         }
         lds_barrier();
@@ -229,16 +262,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     if (r < R) {
         const bool pad = t >= n;
         const float il = pad || l == 0.f ? 0.f : vref / l;
-        if (pa.nsplit == 1) {
-            TO *op = (TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st;
-#pragma unroll
-            for (int d = 0; d < ND; d++)
-#pragma unroll
-                for (int e = 0; e < 16; e++) stf(op, d * 32 + (e / 4) * 8 + hi * 4 + (e & 3), il == 0.f ? 0.f : o[d][e] * il);
-            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = (!pad && l > 0.f && finite(l)) ? m + __builtin_amdgcn_logf(l) - SHIFT : INFINITY;
-        } else {
-            const size_t at = ((size_t)si * pa.nsplit + split) * R + r;
-            float *op = pa.part_o + at * DH;
+        auto put = [&](auto *op) {
 #pragma unroll
             for (int d = 0; d < ND; d++)
 #pragma unroll
@@ -246,8 +270,15 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
                     f4 u;
 #pragma unroll
                     for (int e = 0; e < 4; e++) u[e] = il == 0.f ? 0.f : o[d][q * 4 + e] * il;
-                    *reinterpret_cast<f4 *>(op + d * 32 + q * 8 + hi * 4) = u;
+                    store4(op + d * 32 + q * 8 + hi * 4, u);
                 }
+        };
+        if (pa.nsplit == 1) {
+            put((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st);
+            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = (!pad && l > 0.f && finite(l)) ? m + __builtin_amdgcn_logf(l) - SHIFT : INFINITY;
+        } else {
+            const size_t at = ((size_t)si * pa.nsplit + split) * R + r;
+            put(pa.part_o + at * DH);
             if (hi == 0) { pa.part_ml[at * 2] = m; pa.part_ml[at * 2 + 1] = pad ? 0.f : l; }
         }
     }
@@ -299,14 +330,6 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
                 const uint2 u = *reinterpret_cast<const uint2 *>(a.mem.k + ((size_t)si * a.cap + (size_t)J * BLK + kt * 32 + l32) * DH + k * 16 + hi * 8);
                 kf[kt][k] = codes_to_bf16(u.x, u.y);
             }
-        int ids[2][16];
-#pragma unroll
-        for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const int at = kt * 32 + (e / 4) * 8 + hi * 4 + (e & 3);
-                ids[kt][e] = at < live ? a.mem.idx[(size_t)si * a.cap + (size_t)J * BLK + at] : 0x7FFFFFFF;
-            }
         const float c = a.mem.ks[(size_t)si * a.nblk + J] * a.scale2;
         float acc[2][16];
 #pragma unroll
@@ -316,37 +339,57 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
         // rows from the first token that sees any of the block's pairs
         const int64_t t0 = (int64_t)sp.x > pos0 ? (int64_t)sp.x - pos0 : 0;
         const int rows = n * a.g, first = t0 >= n ? rows : (int)t0 * a.g / 32 * 32;
+        // this lane's row as token and head, moved on by 128 rows at a time; the next row's queries are under way while one is worked on
+        int r = first + w * 32 + l32, t = r / a.g, hd = r - t * a.g;
+        const int t_step = 128 / a.g, h_step = 128 - t_step * a.g;
+        bf8 qf[NK][QP];
+        float st = INFINITY;
+        auto load = [&]() {
+            const TI *qp = (const TI *)a.q + b * a.q_sb + (h * a.g + hd) * a.q_sh + t * a.q_st + hi * 8;
+            st = r < rows ? pa.stat[(size_t)si * R + r] : INFINITY;
+#pragma unroll
+            for (int k = 0; k < NK; k++) {
+                if (r < rows) load_query(qp + k * 16, qf[k]);
+                else zero_query<QP>(qf[k]);
+            }
+        };
+        load();
         for (int r0 = first + w * 32; r0 < rows; r0 += 128) {
-            const int r = r0 + l32, t = r / a.g, hq = h * a.g + (r - t * a.g);
             const int pos = (int)(pos0 + t);
-            const float st = r < rows ? pa.stat[(size_t)si * R + r] : INFINITY;
+            const float off = st;
             f16v s[2];
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
                 for (int e = 0; e < 16; e++) s[kt][e] = 0.f;
 #pragma unroll
-            for (int k = 0; k < NK; k++) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = 0.f;
-                if (r < rows) load8((const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st + k * 16 + hi * 8, x);
-                bf8 qf[QP];
-                split_bf16<QP>(x, qf);
+            for (int k = 0; k < NK; k++)
 #pragma unroll
                 for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-                    for (int p = QP - 1; p >= 0; p--) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kt][k], qf[p], s[kt], 0, 0, 0);
+                    for (int p = QP - 1; p >= 0; p--) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kt][k], qf[k][p], s[kt], 0, 0, 0);
+            const bool masked = (int64_t)sp.y > pos0 + r0 / a.g;      // (slots without a pair count as later than all queries)
+            r += 128; t += t_step; hd += h_step;
+            if (hd >= a.g) { hd -= a.g; t++; }
+            load();
+            // fmaxf drops what rows without weight (off infinite) make of a NaN key
+            if (masked) {
+#pragma unroll
+                for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        const int at = kt * 32 + q * 8 + hi * 4;
+                        const int4 id = *reinterpret_cast<const int4 *>(a.mem.idx + (size_t)si * a.cap + (size_t)J * BLK + at);
+                        const int ids[4] = {id.x, id.y, id.z, id.w};
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (ids[e] > pos || at + e >= live) s[kt][q * 4 + e] = -INFINITY;
+                    }
             }
-            const bool none = st == INFINITY;
-            const bool masked = live < BLK || (int64_t)sp.y > pos0 + r0 / a.g;
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -st));
-                    acc[kt][e] += none || (masked && ids[kt][e] > pos) ? 0.f : p;
-                }
+                for (int e = 0; e < 16; e++) acc[kt][e] += fmaxf(__builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), 0.f);
         }
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)

@@ -2,7 +2,7 @@
 // query head of the group).
 //
 // Bound by HBM: every code is read once for all rows of the group (256 bytes a slot at d = 128 against 2 x 4 x 128 x 2 flops for four heads).
-// A stream's blocks are dealt to `nsplit` workgroups and within one to its four wavefronts; each wavefront keeps a running maximum, sum
+// A stream's blocks are dealt to `nsplit` workgroups and within one to its wavefronts (four, or eight where one workgroup has all of a short cache); each wavefront keeps a running maximum, sum
 // and output of its own over the blocks it reads, nothing is exchanged before its last block.
 //
 // One block (64 slots) of a wavefront:
@@ -27,7 +27,6 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i2 __attribute__((ext_vector_type(2)));
 
-constexpr int STEP_NW = 4;         // wavefronts per workgroup
 constexpr float P_SHIFT = 14.f;    // probabilities are held times 2^14
 
 // eight codes -> eight bf16 (exact)
@@ -78,8 +77,33 @@ struct StepArgs {
 template <int DH>
 __device__ __forceinline__ int vswz(int row) { return (row / (256 / DH)) & (DH / 16 - 1); }
 
-__device__ __forceinline__ float quad_max(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
-__device__ __forceinline__ float quad_sum(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+// this lane's value and that of the lane 16 / 32 away (row swaps, no LDS round trip)
+struct Two { float a, b; };
+__device__ __forceinline__ Two swap_rows16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Two swap_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float half_max(float v) { const Two t = swap_halves(v); return fmaxf(t.a, t.b); }
+__device__ __forceinline__ float half_sum(float v) { const Two t = swap_halves(v); return t.a + t.b; }
+__device__ __forceinline__ float quad_max(float v) { const Two t = swap_rows16(v); return half_max(fmaxf(t.a, t.b)); }
+__device__ __forceinline__ float quad_sum(float v) { const Two t = swap_rows16(v); return half_sum(t.a + t.b); }
+
+// eight query elements as matrix operand parts
+__device__ __forceinline__ void load_query(const bf16_t *p, bf8 *part) { part[0] = *reinterpret_cast<const bf8 *>(p); }
+__device__ __forceinline__ void load_query(const float *p, bf8 *part) {
+    float x[8];
+    load8(p, x);
+    split_bf16<3>(x, part);
+}
+template <int QP>
+__device__ __forceinline__ void zero_query(bf8 *part) {
+#pragma unroll
+    for (int p = 0; p < QP; p++) part[p] = __builtin_bit_cast(bf8, make_uint4(0, 0, 0, 0));
+}
 
 // Puts the stream's new token into slot c0, by one wavefront: lanes below DH / 8 take eight elements of the key each, as many behind them the value.
 // The same codes, scales and rules as append_kernel.
@@ -133,16 +157,16 @@ __device__ __forceinline__ void append_token(const Args &a, int si, int b, int h
     __threadfence_block();      // this wavefront reads the block back
 }
 
-template <int DH, int CT, typename TI, typename TO, bool MASK, bool APPEND>
-__global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
+template <int DH, int CT, int NW, typename TI, typename TO, bool MASK, bool APPEND>
+__global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
     constexpr int QP = sizeof(TI) == 4 ? 3 : 1, PP = sizeof(TO) == 4 ? 2 : 1;
     constexpr int NK = DH / 32;                     // contraction steps of the first product
     constexpr int ND = DH / 16;                     // tiles of 16 output columns
     constexpr int KB = DH / 4;                      // bytes of a key row per lane: quad q holds pieces c * 64 + q * 16 (DH = 32: q * 8)
     constexpr int VI = DH / 16;                     // 16-byte loads per lane of a block's values
     constexpr int PR = DH / 16;                     // pieces per row
-    __shared__ __attribute__((aligned(16))) uint8_t stage[STEP_NW][BLK * DH];
-    __shared__ float ml_l[STEP_NW][2][16 * CT], vref_l[STEP_NW];
+    __shared__ __attribute__((aligned(16))) uint8_t stage[NW][BLK * DH];
+    __shared__ float ml_l[NW][2][16 * CT], vref_l[NW];
     const Args &a = sa.a;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
     const int si = blockIdx.x, split = blockIdx.y, b = si / a.Hkv, h = si - b * a.Hkv;
@@ -150,14 +174,18 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
     const int nb = (count + BLK - 1) / BLK;
     const int J0 = (int)((int64_t)nb * split / sa.nsplit), J1 = (int)((int64_t)nb * (split + 1) / sa.nsplit);
     // a step's own token goes into the stream's last block, by the wavefront that reads it (nobody else does)
-    if (APPEND && count > c0 && J1 == nb && J1 > J0 && (nb - 1 - J0) % STEP_NW == w) append_token<DH, TI>(a, si, b, h, c0, lane);
+    if (APPEND && count > c0 && J1 == nb && J1 > J0 && (nb - 1 - J0) % NW == w) append_token<DH, TI>(a, si, b, h, c0, lane);
     const uint8_t *kc = a.mem.k + (size_t)si * a.cap * DH, *vc = a.mem.v + (size_t)si * a.cap * DH;
     const float *ks = a.mem.ks + (size_t)si * a.nblk, *vs = a.mem.vs + (size_t)si * a.nblk;
     const int32_t *idx = a.mem.idx + (size_t)si * a.cap;
     const int64_t pos0 = MASK ? a.mem.n_tokens[si] - n : 0;
 
     uint32_t kr[4][KB / 4], vr[VI * 4];
-    float ksJ = 0.f, vsJ = 0.f;
+    float ksT = 0.f, vsT = 0.f;       // scales of this wavefront's next 64 blocks, one per lane (a scalar load would make each LDS wait longer)
+    auto scales = [&](int J) {
+        const int x = min(J + NW * lane, a.nblk - 1);
+        ksT = ks[x]; vsT = vs[x];
+    };
     int4 id[4];
     auto load = [&](int J) {
         const uint8_t *kp = kc + (size_t)J * BLK * DH, *vp = vc + (size_t)J * BLK * DH;
@@ -180,12 +208,11 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
             const uint4 u = *reinterpret_cast<const uint4 *>(vp + i * 1024 + lane * 16);
             vr[4 * i] = u.x; vr[4 * i + 1] = u.y; vr[4 * i + 2] = u.z; vr[4 * i + 3] = u.w;
         }
-        ksJ = ks[J]; vsJ = vs[J];
         if (MASK)
 #pragma unroll
             for (int t = 0; t < 4; t++) id[t] = *reinterpret_cast<const int4 *>(idx + (size_t)J * BLK + t * 16 + quad * 4);
     };
-    if (J0 + w < J1) load(J0 + w);
+    if (J0 + w < J1) { scales(J0 + w); load(J0 + w); }
 
     // queries of row 16 ct + n16 in the keys' order of columns
     bf8 qf[CT][NK][QP];
@@ -197,11 +224,8 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
         const TI *qp = (const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st;
 #pragma unroll
         for (int s = 0; s < NK; s++) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) x[e] = 0.f;
-            if (t < n) load8(qp + (DH == 32 ? quad * 8 : (s / 2) * 64 + quad * 16 + (s & 1) * 8), x);
-            split_bf16<QP>(x, qf[ct][s]);
+            if (t < n) load_query(qp + (DH == 32 ? quad * 8 : (s / 2) * 64 + quad * 16 + (s & 1) * 8), qf[ct][s]);
+            else zero_query<QP>(qf[ct][s]);
         }
     }
     f4 o[CT][ND];
@@ -213,7 +237,9 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
         for (int c = 0; c < ND; c++) o[ct][c] = (f4){0.f, 0.f, 0.f, 0.f};
     }
     uint8_t *st = stage[w];
-    for (int J = J0 + w; J < J1; J += STEP_NW) {
+    for (int J = J0 + w, it = 0; J < J1; J += NW, it++) {
+        if (it == 64) { it = 0; scales(J); }
+        const float ksJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksT), it)), vsJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsT), it));
         const int live = count - J * BLK;          // slots of this block that hold pairs (64 and more: all)
         const float c = ksJ * a.scale2, vnew = fmaxf(vref, vsJ), vscale = vsJ / vnew, vkeep = vref / vnew;
         vref = vnew;
@@ -240,7 +266,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
             }
         }
         const int4 idJ[4] = {id[0], id[1], id[2], id[3]};
-        if (J + STEP_NW < J1) load(J + STEP_NW);
+        if (J + NW < J1) load(J + NW);
         h8 pf[CT][2][PP];
 #pragma unroll
         for (int ct = 0; ct < CT; ct++) {
@@ -294,7 +320,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
         }
     }
 
-    // the four wavefronts' shares: O^T [column][row] in turn through the staging memory, weighted by their maxima
+    // the wavefronts' shares: O^T [column][row] in turn through the staging memory, weighted by their maxima
     if (lane == 0) vref_l[w] = vref;
     if (quad == 0)
 #pragma unroll
@@ -313,16 +339,16 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
 #pragma unroll
             for (int e = 0; e < 4; e++) ol[(w * DH + d * 16 + quad * 4 + e) * 16 + n16] = o[ct][d][e];
         __syncthreads();
-        for (int e = tid; e < 16 * DH; e += 256) {
+        for (int e = tid; e < 16 * DH; e += 64 * NW) {
             const int r16 = e / DH, col = e - r16 * DH, r = ct * 16 + r16;
             if (r >= R) continue;
             float M = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < STEP_NW; i++) M = fmaxf(M, ml_l[i][0][r]);
+            for (int i = 0; i < NW; i++) M = fmaxf(M, ml_l[i][0][r]);
             const float mu = M == -INFINITY ? 0.f : M;
-            float L = 0.f, f[STEP_NW], y = 0.f;
+            float L = 0.f, f[NW], y = 0.f;
 #pragma unroll
-            for (int i = 0; i < STEP_NW; i++) {
+            for (int i = 0; i < NW; i++) {
                 f[i] = __builtin_amdgcn_exp2f(ml_l[i][0][r] - mu);
                 L += ml_l[i][1][r] * f[i];
             }
@@ -331,7 +357,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs sa) {
             if (L != 0.f) {
                 const float iL = 1.f / L;
 #pragma unroll
-                for (int i = 0; i < STEP_NW; i++) y += ol[(i * DH + col) * 16 + r16] * f[i] * iL * vref_l[i];
+                for (int i = 0; i < NW; i++) y += ol[(i * DH + col) * 16 + r16] * f[i] * iL * vref_l[i];
             }
             if (sa.nsplit == 1) stf((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st, col, y);
             else sa.part_o[(((size_t)si * sa.nsplit + split) * R + r) * DH + col] = y;
