@@ -66,7 +66,7 @@ inline size_t step_rows(int head_dim) { return head_dim == 256 ? 16 : 32; }
 constexpr int PROMPT_NW = 4;       // wavefronts (of 32 rows) per workgroup of the prompt kernel
 
 struct AttendPlan {
-    bool step, wide;    // wide: one workgroup of eight wavefronts has all of a stream
+    bool step, wide, span;    // wide: one workgroup of eight wavefronts has all of a stream; span: the blocks' index ranges are taken beforehand
     int nsplit, ntiles;
     size_t off_stat, off_o, off_ml, off_logit, off_counts, off_span, bytes;
 };
@@ -94,7 +94,10 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
         // two workgroups fit a compute unit; fewer are split over the blocks, four blocks each at least when the cache is full
         const size_t wgs = S * p.ntiles, most = std::max((size_t)1, (size_t)c->capacity / BLK / 4);
         p.nsplit = (int)(wgs >= 2 * CHIP_CUS ? 1 : std::min(most, (2 * CHIP_CUS + wgs - 1) / wgs));
-        p.off_span = off; off += up(S * (c->capacity / BLK) * 8);
+        // (a launch of its own, 3 us, against 16 loads per lane in every workgroup: at 5 blocks a call of 27 us takes 23 without it, at 64
+        // blocks and 4096 workgroups one of 649 us takes 659)
+        p.span = gather || c->capacity / BLK > 16;
+        p.off_span = off; if (p.span) off += up(S * (c->capacity / BLK) * 8);
         p.off_o = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * c->head_dim * 4);
         p.off_ml = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * 2 * 4);
         p.off_stat = off; if (gather) off += up(S * R * 4);
@@ -169,7 +172,7 @@ lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *
 #undef STEP3
 #undef STEP
         LAUNCH_CHECK();
-        const int jo = p.nsplit > 1 ? R : 0, jw = gather ? std::min((a.cap + 255) / 256, 4096) : 0;
+        const int jo = p.nsplit > 1 ? R : 0, jw = gather ? std::min((a.cap + 1023) / 1024, 4096) : 0;
         if (jo + jw) {
             hipLaunchKernelGGL((step_join_kernel<DH, TO>), dim3(S, jo + jw), dim3(256), 0, stream, sa, jo);
             LAUNCH_CHECK();
@@ -178,14 +181,16 @@ lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *
     }
     PromptArgs pa;
     pa.a = a; pa.nsplit = p.nsplit; pa.ntiles = p.ntiles;
-    pa.span = (int2 *)(ws + p.off_span);
+    pa.span = p.span ? (int2 *)(ws + p.off_span) : nullptr;
     pa.part_o = p.nsplit > 1 ? (float *)(ws + p.off_o) : nullptr;
     pa.part_ml = p.nsplit > 1 ? (float *)(ws + p.off_ml) : nullptr;
     pa.stat = gather ? (float *)(ws + p.off_stat) : nullptr;
     const int S = a.B * a.Hkv, R = a.T * a.g;
     constexpr int LDS = 4 * BLK * DH * 2 + 2 * BLK * 4;
-    hipLaunchKernelGGL(span_kernel, dim3(std::min((a.nblk + 3) / 4, 256), S), dim3(256), 0, stream, pa);
-    LAUNCH_CHECK();
+    if (p.span) {
+        hipLaunchKernelGGL(span_kernel, dim3(std::min((a.nblk + 3) / 4, 256), S), dim3(256), 0, stream, pa);
+        LAUNCH_CHECK();
+    }
     hipLaunchKernelGGL((prompt_kernel<DH, PROMPT_NW, TI, TO>), dim3((unsigned)S * p.ntiles * p.nsplit), dim3(64 * PROMPT_NW), LDS, stream, pa);
     LAUNCH_CHECK();
     if (p.nsplit > 1) {
@@ -339,13 +344,13 @@ lola_status lola_full_evict(const lola_full_config *c, const lola_full_state *st
     else hipLaunchKernelGGL((evict_select_kernel<1024>), dim3(S), dim3(1024), lds, (hipStream_t)stream, a);
     LAUNCH_CHECK();
     if (p.nkb == 0) return LOLA_OK;
-    const dim3 grid(p.nkb, S);
-    switch (a.d) {
-        case 32: hipLaunchKernelGGL((evict_move_kernel<32>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
-        case 64: hipLaunchKernelGGL((evict_move_kernel<64>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
-        case 128: hipLaunchKernelGGL((evict_move_kernel<128>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
-        default: hipLaunchKernelGGL((evict_move_kernel<256>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
-    }
+    // Up to eight pairs a block on average: one wavefront per block (128 sequences of the 1B shape back to 1111 pairs after 16 tokens 18 us with
+    // four); beyond, four (32 Ki pairs cut to 2048).
+    const bool few = p.most <= 8 * p.nkb;
+    const dim3 grid(few ? (p.nkb + 3) / 4 : p.nkb, S);
+#define MOVE(DH) (few ? evict_move_kernel<DH, 1> : evict_move_kernel<DH, 4>)
+    hipLaunchKernelGGL((a.d == 32 ? MOVE(32) : a.d == 64 ? MOVE(64) : a.d == 128 ? MOVE(128) : MOVE(256)), grid, dim3(256), 0, (hipStream_t)stream, a);
+#undef MOVE
     LAUNCH_CHECK();
     return LOLA_OK;
 }

@@ -35,6 +35,9 @@ struct Args {
 
 __device__ __forceinline__ int exponent_of(float scale) { return (int)((__float_as_uint(scale) >> 23) & 255u) - 127; }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+// 1 / x for a power of two (2^-126 .. 2^126)
+__device__ __forceinline__ float inv_pow2(float x) { return __uint_as_float(0x7F000000u - (__float_as_uint(x) & 0x7F800000u)); }
+
 // least e >= EXP_MIN with a <= 448 * 2^e, a >= 0 finite: 448 = 1.75 * 2^8, a = 1.f * 2^x (a below 2^-126 is below every bound)
 __device__ __forceinline__ int fit_exponent(float a) {
     const uint32_t u = __float_as_uint(a);
@@ -333,64 +336,98 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
     }
 }
 
-// One workgroup per block below the budget: the pairs that move into it come from slots at and beyond `keep`, which no workgroup writes.
-// (Of the block that the budget ends in only rows below it are rescaled; its scales, which other workgroups read as a
-// source's, are read from the copy taken beforehand.)
-template <int DH>
+// The pairs that move into a block below the budget come from slots at and beyond `keep`, which no workgroup writes.  (Of the block
+// that the budget ends in only rows below it are rescaled; its scales, which others read as a source's, are read from the copy
+// taken beforehand.)  WPB wavefronts take a block: four where many pairs move, one (four blocks per workgroup) where few do.  Up to four
+// passes over the rows are held in registers between finding the exponent and writing.
+template <int DH, int WPB>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
-    constexpr int TPR = DH / 8, RPP = 256 / TPR;
+    constexpr int TPR = DH / 8, RPP = 64 * WPB / TPR, U = 4;      // threads per row, rows per pass, passes held
     __shared__ float red[2][4];
-    const int si = blockIdx.y, J = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int si = blockIdx.y, w = threadIdx.x >> 6, lane = threadIdx.x & 63, tid = WPB == 4 ? threadIdx.x : lane;
+    const int J = WPB == 4 ? blockIdx.x : blockIdx.x * 4 + w;
+    if (J >= a.nkb) return;      // (with one wavefront per block there is no workgroup barrier)
     const int j0 = a.before[(size_t)si * (a.nkb + 1) + J], j1 = a.before[(size_t)si * (a.nkb + 1) + J + 1];
     if (j0 >= j1) return;
     const int32_t *dst = a.dst + (size_t)si * a.most, *src = a.src + (size_t)si * a.most;
     const size_t base = (size_t)si * a.cap;
     const int col = (tid % TPR) * 8;
-    auto scale = [&](const float *p, int s, int which) {
-        return a.keep % BLK && s / BLK == a.keep / BLK ? a.edge[2 * si + which] : p[(size_t)si * a.nblk + s / BLK];
+    const float ok_s = a.mem.ks[(size_t)si * a.nblk + J], ov_s = a.mem.vs[(size_t)si * a.nblk + J];
+    const float edge_k = a.edge[2 * si], edge_v = a.edge[2 * si + 1];
+    uint2 kc[U], vc[U];
+    float sk[U], sv[U];
+    int from[U];
+    auto load = [&](int jb) {
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int j = jb + u * RPP + tid / TPR;
+            from[u] = j < j1 ? src[j] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int s = from[u];
+            kc[u] = vc[u] = make_uint2(0, 0); sk[u] = sv[u] = 0.f;
+            if (s < 0) continue;
+            kc[u] = *reinterpret_cast<const uint2 *>(a.mem.k + (base + s) * DH + col);
+            vc[u] = *reinterpret_cast<const uint2 *>(a.mem.v + (base + s) * DH + col);
+            const bool edge = a.keep % BLK && s / BLK == a.keep / BLK;
+            sk[u] = edge ? edge_k : a.mem.ks[(size_t)si * a.nblk + s / BLK];
+            sv[u] = edge ? edge_v : a.mem.vs[(size_t)si * a.nblk + s / BLK];
+        }
     };
     float ak = 0.f, av = 0.f;
-    for (int j = j0 + tid / TPR; j < j1; j += RPP) {
-        const int s = src[j];
-        const uint2 kc = *reinterpret_cast<const uint2 *>(a.mem.k + (base + s) * DH + col), vc = *reinterpret_cast<const uint2 *>(a.mem.v + (base + s) * DH + col);
-        float x[8], mk = 0.f, mv = 0.f;
-        from_codes(kc.x, x); from_codes(kc.y, x + 4);
+    for (int jb = j0; jb < j1; jb += U * RPP) {
+        load(jb);
 #pragma unroll
-        for (int e = 0; e < 8; e++) mk = fmaxf(mk, fabsf(x[e]));   // (a NaN key counts as zero)
-        from_codes(vc.x, x); from_codes(vc.y, x + 4);
+        for (int u = 0; u < U; u++) {
+            float x[8], mk = 0.f, mv = 0.f;
+            from_codes(kc[u].x, x); from_codes(kc[u].y, x + 4);
 #pragma unroll
-        for (int e = 0; e < 8; e++) mv = fmaxf(mv, fabsf(x[e]));
-        ak = fmaxf(ak, mk * scale(a.mem.ks, s, 0));
-        av = fmaxf(av, mv * scale(a.mem.vs, s, 1));
+            for (int e = 0; e < 8; e++) mk = fmaxf(mk, fabsf(x[e]));   // (a NaN key counts as zero)
+            from_codes(vc[u].x, x); from_codes(vc[u].y, x + 4);
+#pragma unroll
+            for (int e = 0; e < 8; e++) mv = fmaxf(mv, fabsf(x[e]));
+            ak = fmaxf(ak, mk * sk[u]);
+            av = fmaxf(av, mv * sv[u]);
+        }
     }
     ak = wave_max(ak); av = wave_max(av);
-    if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
-    const float ok_s = a.mem.ks[(size_t)si * a.nblk + J], ov_s = a.mem.vs[(size_t)si * a.nblk + J];
-    __syncthreads();
-    ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-    av = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+    if (WPB == 4) {
+        if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
+        __syncthreads();
+        ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+        av = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+    }
     const int ok = exponent_of(ok_s), ov = exponent_of(ov_s), ek = max(ok, fit_exponent(ak)), ev = max(ov, fit_exponent(av));
     uint8_t *kb = a.mem.k + (base + (size_t)J * BLK) * DH, *vb = a.mem.v + (base + (size_t)J * BLK) * DH;
     if (ek > ok || ev > ov) {
         const float fk = pow2(max(ok - ek, -40)), fv = pow2(max(ov - ev, -40));
         const int rows = min(BLK, a.keep - J * BLK);
-        for (int e = tid; e < rows * TPR; e += 256) {
+        for (int e = tid; e < rows * TPR; e += 64 * WPB) {
             if (ek > ok) { uint2 u = reinterpret_cast<uint2 *>(kb)[e]; u.x = rescale_codes(u.x, fk); u.y = rescale_codes(u.y, fk); reinterpret_cast<uint2 *>(kb)[e] = u; }
             if (ev > ov) { uint2 u = reinterpret_cast<uint2 *>(vb)[e]; u.x = rescale_codes(u.x, fv); u.y = rescale_codes(u.y, fv); reinterpret_cast<uint2 *>(vb)[e] = u; }
         }
         if (tid == 0) { a.mem.ks[(size_t)si * a.nblk + J] = pow2(ek); a.mem.vs[(size_t)si * a.nblk + J] = pow2(ev); }
-        __syncthreads();   // the rows that the moved pairs replace were rescaled by other threads
+        // the rows that the moved pairs replace were rescaled by other threads
+        if (WPB == 4) __syncthreads(); else __threadfence_block();
     }
-    for (int j = j0 + tid / TPR; j < j1; j += RPP) {
-        const int s = src[j], t = dst[j];
-        uint2 kc = *reinterpret_cast<const uint2 *>(a.mem.k + (base + s) * DH + col), vc = *reinterpret_cast<const uint2 *>(a.mem.v + (base + s) * DH + col);
-        // (a source's exponent may be larger than the block's: its codes then grow, and fit by the choice of ek, ev)
-        const float fk = pow2(min(40, max(exponent_of(scale(a.mem.ks, s, 0)) - ek, -40))), fv = pow2(min(40, max(exponent_of(scale(a.mem.vs, s, 1)) - ev, -40)));
-        kc.x = rescale_codes(kc.x, fk); kc.y = rescale_codes(kc.y, fk);
-        vc.x = rescale_codes(vc.x, fv); vc.y = rescale_codes(vc.y, fv);
-        *reinterpret_cast<uint2 *>(a.mem.k + (base + t) * DH + col) = kc;
-        *reinterpret_cast<uint2 *>(a.mem.v + (base + t) * DH + col) = vc;
-        if (tid % TPR == 0) { a.mem.idx[base + t] = a.mem.idx[base + s]; a.mem.weight[base + t] = a.mem.weight[base + s]; }
+    for (int jb = j0; jb < j1; jb += U * RPP) {
+        if (j1 - j0 > U * RPP) load(jb);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int s = from[u];
+            if (s < 0) continue;
+            const int t = dst[jb + u * RPP + tid / TPR];
+            // (a source's exponent may be larger than the block's: its codes then grow, and fit by the choice of ek, ev)
+            const float fk = pow2(min(40, max(exponent_of(sk[u]) - ek, -40))), fv = pow2(min(40, max(exponent_of(sv[u]) - ev, -40)));
+            uint2 c = kc[u];
+            c.x = rescale_codes(c.x, fk); c.y = rescale_codes(c.y, fk);
+            *reinterpret_cast<uint2 *>(a.mem.k + (base + t) * DH + col) = c;
+            c = vc[u];
+            c.x = rescale_codes(c.x, fv); c.y = rescale_codes(c.y, fv);
+            *reinterpret_cast<uint2 *>(a.mem.v + (base + t) * DH + col) = c;
+            if (tid % TPR == 0) { a.mem.idx[base + t] = a.mem.idx[base + s]; a.mem.weight[base + t] = a.mem.weight[base + s]; }
+        }
     }
 }
 

@@ -7,10 +7,11 @@
 // relative to the largest scale so far (both exact, up to fp16's range).  Products are 32x32x16 and transposed: S^T = K Q^T has a query per
 // lane pair, so the running maximum and sum live there, and its C layout is the B layout of O^T += V^T P^T, whose V^T comes from the
 // transposing 16-bit LDS read.  Which blocks can be passed over and which need a comparison per element follows from the least and largest token
-// index of each block, taken beforehand by a kernel of its own: slots need not be in the order of tokens (evictions fill holes).
+// index of each block (of long caches taken beforehand by a kernel of its own): slots need not be in the order of tokens (evictions fill holes).
 //
 // The maximum is only moved when a logit exceeds it by more than 2^RAISE: weights then reach 2^RAISE, held times 2^SHIFT in fp16.
 #pragma once
+#include <type_traits>
 #include "full_step.h"
 
 namespace lola {
@@ -24,7 +25,7 @@ constexpr float RAISE = 8.f, SHIFT = 7.f;
 struct PromptArgs {
     Args a;
     int nsplit, ntiles;
-    int2 *span;        // [S][nblk] least and largest token index of each block
+    int2 *span;        // [S][nblk] least and largest token index of each block; NULL: up to 64 blocks, each workgroup looks at the indices
     float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
     float *part_ml;    // [S][nsplit][R][2] maximum (powers of two) and sum
     float *stat;       // [S][R] maximum + log2 of the sum (infinite: the row adds no weight), where weights are gathered
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     const uint8_t *kc = a.mem.k + (size_t)si * a.cap * DH, *vc = a.mem.v + (size_t)si * a.cap * DH;
     const float *ks = a.mem.ks + (size_t)si * a.nblk, *vs = a.mem.vs + (size_t)si * a.nblk;
     const int32_t *idx = a.mem.idx + (size_t)si * a.cap;
-    const int2 *span = pa.span + (size_t)si * a.nblk;
+    const int2 *span = pa.span ? pa.span + (size_t)si * a.nblk : nullptr;
     const int nb = (count + BLK - 1) / BLK;
     const int J0 = (int)((int64_t)nb * split / pa.nsplit), J1 = (int)((int64_t)nb * (split + 1) / pa.nsplit);
     // What is known of 64 blocks from `base` on, one per lane, and which of them any query of the workgroup sees.  (Read block by
@@ -100,6 +101,26 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         const int x = min(J + lane, a.nblk - 1);
         spT = span[x]; ksT = ks[x]; vsT = vs[x];
         seen = __ballot(J + lane < J1 && (int64_t)spT.x <= wg_last);
+    };
+    // the same from the indices themselves (short caches, up to 64 blocks: one launch less), a block per lane
+    auto table_of_indices = [&]() {
+        base = J0;
+        const int x = min(J0 + lane, a.nblk - 1), live = count - x * BLK;
+        int lo = 0x7FFFFFFF, hi2 = live < BLK ? 0x7FFFFFFF : 0;
+        if (J0 + lane < J1) {
+            const int4 *ip = reinterpret_cast<const int4 *>(idx + (size_t)x * BLK);
+#pragma unroll
+            for (int q = 0; q < BLK / 4; q++) {
+                const int4 id = ip[q];
+                if (q * 4 < live) lo = min(lo, id.x);
+                if (q * 4 + 1 < live) lo = min(lo, id.y);
+                if (q * 4 + 2 < live) lo = min(lo, id.z);
+                if (q * 4 + 3 < live) lo = min(lo, id.w);
+                hi2 = max(hi2, max(max(id.x, id.y), max(id.z, id.w)));
+            }
+        }
+        spT = make_int2(lo, hi2); ksT = ks[x]; vsT = vs[x];
+        seen = __ballot(J0 + lane < J1 && (int64_t)lo <= wg_last);
     };
     auto lane_of = [&](int v, int J) { return __builtin_amdgcn_readlane(v, J - base); };
     auto lane_of_f = [&](float v, int J) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), J - base)); };
@@ -155,8 +176,11 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             }
     };
 
-    int cur = 0, J = J1;
-    if (J0 < J1) { table(J0); J = next(J0); }
+    int J = J1;
+    if (J0 < J1) {
+        if (span) table(J0); else table_of_indices();
+        J = next(J0);
+    }
     float vref = 0.f, vstage = 0.f, c = 0.f;      // o is in units of vref; the staged block's values in units of vstage
     bool masked = false;
     if (J < J1) {
@@ -167,10 +191,11 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         store(lds, J, 1.f);
     }
     lds_barrier();
-    while (J < J1) {
+    auto block = [&](auto which) {
+        constexpr int CUR = decltype(which)::value;
         const int Jn = next(J + 1);
         if (Jn < J1) load(Jn);
-        const uint8_t *kb = lds + cur * BUF;
+        const uint8_t *kb = lds + CUR * BUF;
         const _Float16 *vb = reinterpret_cast<const _Float16 *>(kb + HALF);
         f16v s[2];
 #pragma unroll
@@ -212,7 +237,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             for (int d = 0; d < ND; d++) o[d] *= f;
         }
         if (vstage > vref) {      // (uniform; rare beyond the first block)
-            const float f = vref / vstage;
+            const float f = vref * inv_pow2(vstage);
 #pragma unroll
             for (int d = 0; d < ND; d++) o[d] *= f;
             vref = vstage;
@@ -253,10 +278,15 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             vstage = fmaxf(vstage, v);
             c = lane_of_f(ksT, Jn) * a.scale2;
             masked = (int64_t)lane_of(spT.y, Jn) > w_first;
-            store(lds + (cur ^ 1) * BUF, Jn, v / vstage);
+            store(lds + (CUR ^ 1) * BUF, Jn, v * inv_pow2(vstage));
         }
         lds_barrier();
-        J = Jn; cur ^= 1;
+        J = Jn;
+    };
+    while (J < J1) {      // (twice, so that each buffer's addresses are constants)
+        block(std::integral_constant<int, 0>());
+        if (J >= J1) break;
+        block(std::integral_constant<int, 1>());
     }
     l = half_sum(l);
     if (r < R) {

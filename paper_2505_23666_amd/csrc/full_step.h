@@ -241,7 +241,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
         if (it == 64) { it = 0; scales(J); }
         const float ksJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksT), it)), vsJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsT), it));
         const int live = count - J * BLK;          // slots of this block that hold pairs (64 and more: all)
-        const float c = ksJ * a.scale2, vnew = fmaxf(vref, vsJ), vscale = vsJ / vnew, vkeep = vref / vnew;
+        const float c = ksJ * a.scale2, vnew = fmaxf(vref, vsJ), iv = inv_pow2(vnew), vscale = vsJ * iv, vkeep = vref * iv;
         vref = vnew;
         // values to LDS; slots without a pair hold zeros there
 #pragma unroll
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
 }
 
 // Joins the shares: workgroup y < jo of a stream one row of outputs (DH / 4 threads per share, the shares dealt to the groups of threads); the
-// others, where weights are gathered, add sum over rows of 2^(logit - M) / L to the weights of 256 slots at a time.
+// others, where weights are gathered, add sum over rows of 2^(logit - M) / L to the weights of 1024 slots at a time.
 template <int DH, typename TO>
 __global__ __launch_bounds__(256) void step_join_kernel(StepArgs sa, int jo) {
     const Args &a = sa.a;
@@ -426,7 +426,7 @@ __global__ __launch_bounds__(256) void step_join_kernel(StepArgs sa, int jo) {
         return;
     }
     const int n = new_tokens(a, b), count = sa.append ? sa.counts[si] : n ? held(a, si) : 0;
-    if ((y - jo) * 256 >= count) return;
+    if ((y - jo) * 1024 >= count) return;
     // eight lanes per row look at the shares
     const int r8 = tid >> 3, j = tid & 7;
     if (r8 < R) {
@@ -439,13 +439,21 @@ __global__ __launch_bounds__(256) void step_join_kernel(StepArgs sa, int jo) {
         if (j == 0) { M_l[r8] = mu; L_l[r8] = L > 0.f && finite(L) ? 1.f / (L * SCALE) : 0.f; }
     }
     __syncthreads();
-    for (int slot = (y - jo) * 256 + tid; slot < count; slot += (gridDim.y - jo) * 256) {
-        float acc = 0.f;
+    // four slots per thread (the logits of slots without a pair are -inf or were never written: masked)
+    for (int slot = ((y - jo) * 256 + tid) * 4; slot < count; slot += (gridDim.y - jo) * 1024) {
+        f4 acc = (f4){0.f, 0.f, 0.f, 0.f};
         for (int r = 0; r < n * a.g; r++) {
-            const float f = L_l[r];
-            if (f != 0.f) acc += __builtin_amdgcn_exp2f(sa.logit[((size_t)si * R + r) * a.cap + slot] - M_l[r]) * f;
+            const float f = L_l[r], m = M_l[r];
+            const f4 s = *reinterpret_cast<const f4 *>(sa.logit + ((size_t)si * R + r) * a.cap + slot);
+            if (f != 0.f)
+#pragma unroll
+                for (int e = 0; e < 4; e++) acc[e] += __builtin_amdgcn_exp2f(s[e] - m) * f;
         }
-        a.mem.weight[(size_t)si * a.cap + slot] += acc;
+        float *wp = a.mem.weight + (size_t)si * a.cap + slot;
+        const f4 was = *reinterpret_cast<const f4 *>(wp);
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (slot + e < count) wp[e] = was[e] + acc[e];
     }
 }
 
