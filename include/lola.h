@@ -301,7 +301,7 @@ lola_status lola_full_append(const lola_full_config *cfg, const lola_full_state 
  *   y_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j) / sum_j exp(scale q_i.k_j).
  * A query that sees nothing, and the rows i >= n, get zeros.
  * gather = 1 adds sum over the group's query heads and i < n of p_ij to weight[j]; queries whose output is NaN add nothing.
- * q, out [B, Hq, T, d] (or tokens first).  T >= 0; T * (Hq / Hkv) at most 2^24.
+ * q, out [B, Hq, T, d] (or tokens first).  T >= 0; T * (Hq / Hkv) at most 2^24, B * Hq * T at most 2^30 (also in lola_full_append).
  */
 lola_status lola_full_attend(const lola_full_config *cfg, const lola_full_state *st, const void *q, const int32_t *lens,
                              int32_t T, int32_t gather, void *out, void *workspace, size_t workspace_bytes, void *stream);

@@ -314,7 +314,11 @@ class LolaFullCache:
 
     capacity is rounded up to whole blocks of 64 slots.  buffers: the tensors of an existing cache by name (k, v float8_e4m3fn
     [B, Hkv, capacity, d], k_scale, v_scale, idx, weight, count, n_tokens), used in place and not emptied; weights=False
-    leaves `weight` out: such a cache can neither gather weights nor evict."""
+    leaves `weight` out: such a cache can neither gather weights nor evict.
+
+    append and step refuse tokens that do not fit.  The counts are on the device, so the host keeps a bound of its own (`fill`) and reads
+    them back, which synchronises, only when that is used up; once a call was captured into a graph, whose replays it does not
+    see, before every call outside of one.  In a graph the caller makes sure that tokens fit: the library stores only those that do."""
 
     FIELDS = ("k", "v", "k_scale", "v_scale", "idx", "weight", "count", "n_tokens")
 
@@ -352,6 +356,8 @@ class LolaFullCache:
         self.workspace = None
         self._ws_bytes = {}
         self._q1, self._k1 = (B, Hq, d), (B, Hkv, d)
+        self._outgrown = []     # smaller workspaces: graphs and other streams may still use them
+        self._captured = False
         self.fill = 0 if buffers is None else cap   # at least as many slots as any stream has in use
         if buffers is None:
             self.reset()
@@ -365,20 +371,31 @@ class LolaFullCache:
     def reset(self):
         """Empty caches."""
         self._on_device(lola_full_init, self.cfg, self.st)
-        self.fill = 0
+        self._shrunk(0)
+
+    def _shrunk(self, fill):
+        if torch.cuda.is_current_stream_capturing():
+            self._captured = True
+        else:
+            self.fill = min(self.fill, fill)
 
     def _ws(self, T, gather):
         want = self._ws_bytes.get((T, gather))
         if want is None:
             want = self._ws_bytes[T, gather] = lola_full_workspace_bytes(self.cfg, T, gather)
         if self.workspace is None or self.workspace.numel() < want:
+            if self.workspace is not None:
+                self._outgrown.append(self.workspace)
+                want = max(want, 2 * self.workspace.numel())     # (all outgrown ones together are no larger than the last)
             self.workspace = torch.empty(max(want, 16), dtype=torch.uint8, device=self.device)
         return self.workspace
 
     def _room(self, T, lens):
-        """Raises where a sequence's tokens would not fit.  The counts are read back only when the host's own count of slots is
-        used up (never while a graph is captured: replays are the caller's to count)."""
-        if self.fill + T > self.capacity and not torch.cuda.is_current_stream_capturing():
+        """Raises where a sequence's tokens would not fit."""
+        if torch.cuda.is_current_stream_capturing():
+            self._captured = True
+            return
+        if self._captured or self.fill + T > self.capacity:
             new = T if lens is None else lens.clamp(0, T)[:, None]
             if int((self.count + new).max()) > self.capacity:
                 raise LolaError(f"lola_full_append: the cache's {self.capacity} slots are used up: evict first")
@@ -437,13 +454,10 @@ class LolaFullCache:
         return out
 
     def _step(self, q, k, v, out, gather):
-        if self.fill < self.capacity:
-            self.fill += 1
-        else:
-            self._room(1, None)
+        self._room(1, None)
         lola_full_step(self.cfg, self.st, q, k, v, gather, out, self._ws(1, gather))
 
     def evict(self, keep, first=0, recent=0):
         """Cut every stream to `keep` pairs: the first `first` and the most recent `recent` tokens, then those of largest weight."""
         self._on_device(lola_full_evict, self.cfg, self.st, int(keep), int(first), int(recent), self._ws(0, 0))
-        self.fill = min(self.fill, keep)
+        self._shrunk(int(keep))

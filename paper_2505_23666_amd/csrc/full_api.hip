@@ -35,9 +35,9 @@ lola_status check_state(const lola_full_state *st) {
     return LOLA_OK;
 }
 
-// (2^31 query rows in all is also what one grid dimension of the prompt kernel takes)
+// (2^30 query rows in all are 2^23 workgroups of the prompt kernel and 2^31 threads of one grid dimension)
 bool rows_ok(const lola_full_config *c, int32_t T) {
-    return T >= 0 && (long long)T * (c->n_q_heads / c->n_kv_heads) <= (1 << 24) && (long long)T * c->batch * c->n_q_heads < (1ll << 31);
+    return T >= 0 && (long long)T * (c->n_q_heads / c->n_kv_heads) <= (1 << 24) && (long long)T * c->batch * c->n_q_heads <= (1ll << 30);
 }
 
 Mem make_mem(const lola_full_state *st) {

@@ -244,6 +244,10 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
         for (int J = tid; J <= a.nkb; J += NT) before[J] = 0;
         return;
     }
+    if (a.keep == 0) {      // nothing to rank
+        if (tid == 0) a.mem.count[si] = 0;
+        return;
+    }
     const size_t base = (size_t)si * a.cap;
     const int64_t recent_from = a.mem.n_tokens[si] - a.recent;
     const bool cached = a.cap <= RANKS_LDS;
@@ -321,8 +325,8 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
         if (s % BLK == 0 && s < a.keep) before[s / BLK] = h_at;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            if (hole[e]) a.dst[(size_t)si * a.most + h_at++] = s + e;
-            if (mover[e]) a.src[(size_t)si * a.most + m_at++] = s + e;
+            if (hole[e] && h_at < a.most) a.dst[(size_t)si * a.most + h_at++] = s + e;
+            if (mover[e] && m_at < a.most) a.src[(size_t)si * a.most + m_at++] = s + e;
         }
         holes += all & 0xFFFF; moved += all >> 16;
     }

@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
                 vr[i] = *reinterpret_cast<const uint4 *>(vp + (i * NTHR + tid) * 16);
             }
     };
-    auto store = [&](uint8_t *buf, int J, float vscale) {
+    auto store = [&](uint8_t *buf, int J, float kscale, float vscale) {
         const int live = count - J * BLK;
         if (tid < BLK) reinterpret_cast<int *>(buf + 2 * HALF)[tid] = tid < live ? idr : 0x7FFFFFFF;    // (no pair: later than all queries)
 #pragma unroll
@@ -168,8 +168,8 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             if (ALL || tid < BLK * TPR) {
                 const int e = i * NTHR + tid, row = e / TPR, pc = (e % TPR) * 2;
                 uint8_t *kp = buf + row * DH * 2, *vp = buf + HALF + row * DH * 2;
-                *reinterpret_cast<bf8 *>(kp + ((pc ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].x, kr[i].y);
-                *reinterpret_cast<bf8 *>(kp + (((pc + 1) ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].z, kr[i].w);
+                *reinterpret_cast<bf8 *>(kp + ((pc ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].x, kr[i].y, kscale);
+                *reinterpret_cast<bf8 *>(kp + (((pc + 1) ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].z, kr[i].w, kscale);
                 if (row >= live) vr[i] = make_uint4(0, 0, 0, 0);      // slots without a pair hold zeros
                 *reinterpret_cast<h8 *>(vp + ((pc ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].x, vr[i].y, vscale);
                 *reinterpret_cast<h8 *>(vp + (((pc + 1) ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].z, vr[i].w, vscale);
@@ -181,14 +181,14 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         if (span) table(J0); else table_of_indices();
         J = next(J0);
     }
-    float vref = 0.f, vstage = 0.f, c = 0.f;      // o is in units of vref; the staged block's values in units of vstage
+    const float c = a.scale2;
+    float vref = 0.f, vstage = 0.f;      // o is in units of vref; the staged block's values in units of vstage
     bool masked = false;
     if (J < J1) {
         load(J);
         vstage = lane_of_f(vsT, J);
-        c = lane_of_f(ksT, J) * a.scale2;
         masked = (int64_t)lane_of(spT.y, J) > w_first;
-        store(lds, J, 1.f);
+        store(lds, J, lane_of_f(ksT, J), 1.f);
     }
     lds_barrier();
     auto block = [&](auto which) {
@@ -276,9 +276,8 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         if (Jn < J1) {
             const float v = lane_of_f(vsT, Jn);
             vstage = fmaxf(vstage, v);
-            c = lane_of_f(ksT, Jn) * a.scale2;
             masked = (int64_t)lane_of(spT.y, Jn) > w_first;
-            store(lds + (CUR ^ 1) * BUF, Jn, v * inv_pow2(vstage));
+            store(lds + (CUR ^ 1) * BUF, Jn, lane_of_f(ksT, Jn), v * inv_pow2(vstage));
         }
         lds_barrier();
         J = Jn;
@@ -352,15 +351,16 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
         const int2 sp = pa.span[(size_t)si * a.nblk + J];
         const int64_t pos0 = a.mem.n_tokens[si] - n;
         const int live = count - J * BLK;
+        const float kscale = a.mem.ks[(size_t)si * a.nblk + J];
         bf8 kf[2][NK];
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
             for (int k = 0; k < NK; k++) {
                 const uint2 u = *reinterpret_cast<const uint2 *>(a.mem.k + ((size_t)si * a.cap + (size_t)J * BLK + kt * 32 + l32) * DH + k * 16 + hi * 8);
-                kf[kt][k] = codes_to_bf16(u.x, u.y);
+                kf[kt][k] = codes_to_bf16(u.x, u.y, kscale);
             }
-        const float c = a.mem.ks[(size_t)si * a.nblk + J] * a.scale2;
+        const float c = a.scale2;
         float acc[2][16];
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)

@@ -6,7 +6,7 @@
 // and output of its own over the blocks it reads, nothing is exchanged before its last block.
 //
 // One block (64 slots) of a wavefront:
-//   S^T = K Q^T   16x16x32 bf16: the codes are exact in bf16, so are bf16 queries; fp32 queries enter as three bf16 parts (24 bits).  A lane's
+//   S^T = K Q^T   16x16x32 bf16: keys (codes times scale) are exact in bf16, so are bf16 queries; fp32 queries enter as three bf16 parts (24 bits).  A lane's
 //                 operand is eight consecutive bytes of its key row, straight from global memory: the order of the contraction
 //                 index is free as long as the queries are laid out the same.
 //   p = 2^(s - m + 14), rounded to fp16 (fp32 outputs: two fp16 parts): the operand of the second product.  The shift keeps weights down
@@ -29,11 +29,11 @@ typedef int i2 __attribute__((ext_vector_type(2)));
 
 constexpr float P_SHIFT = 14.f;    // probabilities are held times 2^14
 
-// eight codes -> eight bf16 (exact)
-__device__ __forceinline__ bf8 codes_to_bf16(uint32_t a, uint32_t b) {
+// eight codes times their block's scale -> eight bf16 (exact: the keys themselves)
+__device__ __forceinline__ bf8 codes_to_bf16(uint32_t a, uint32_t b, float scale) {
     union { bf8 v; bf2 p[4]; } u;
-    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
-    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
     return u.v;
 }
 // eight codes times a power of two <= 1 -> eight fp16 (exact down to fp16's least number)
@@ -46,22 +46,19 @@ __device__ __forceinline__ h8 codes_to_f16(uint32_t a, uint32_t b, float scale) 
 __device__ __forceinline__ i2 lds_read_tr8(const uint8_t *p) {
     return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i2 *)(p));
 }
-// x as NP bf16 parts whose sum it is (3 parts: 24 bits; bf16 inputs are their own first part)
-template <int NP>
+// x as three bf16 parts whose sum it is: 8 of its 24 bits each, cut off rather than rounded, so that no part overflows
 __device__ __forceinline__ void split_bf16(const float *x, bf8 *part) {
-    float r[8];
 #pragma unroll
-    for (int e = 0; e < 8; e++) r[e] = x[e];
+    for (int e = 0; e < 8; e++) {
+        float r = x[e];
 #pragma unroll
-    for (int p = 0; p < NP; p++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const __bf16 h = (__bf16)r[e];
-            part[p][e] = h;
-            if (p + 1 < NP) r[e] = finite(r[e]) ? r[e] - (float)h : 0.f;
+        for (int p = 0; p < 3; p++) {
+            const uint32_t u = __float_as_uint(r) & 0xFFFF0000u;
+            part[p][e] = __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
+            r = finite(r) ? r - __uint_as_float(u) : 0.f;      // (NaN and infinities stay in the first part; a NaN may become infinite there: its row is NaN all the same)
         }
+    }
 }
-// (a product of NaN or infinite queries stays NaN or infinite through the first part alone)
 
 struct StepArgs {
     Args a;
@@ -97,7 +94,7 @@ __device__ __forceinline__ void load_query(const bf16_t *p, bf8 *part) { part[0]
 __device__ __forceinline__ void load_query(const float *p, bf8 *part) {
     float x[8];
     load8(p, x);
-    split_bf16<3>(x, part);
+    split_bf16(x, part);
 }
 template <int QP>
 __device__ __forceinline__ void zero_query(bf8 *part) {
@@ -241,7 +238,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
         if (it == 64) { it = 0; scales(J); }
         const float ksJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksT), it)), vsJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsT), it));
         const int live = count - J * BLK;          // slots of this block that hold pairs (64 and more: all)
-        const float c = ksJ * a.scale2, vnew = fmaxf(vref, vsJ), iv = inv_pow2(vnew), vscale = vsJ * iv, vkeep = vref * iv;
+        const float c = a.scale2, vnew = fmaxf(vref, vsJ), iv = inv_pow2(vnew), vscale = vsJ * iv, vkeep = vref * iv;
         vref = vnew;
         // values to LDS; slots without a pair hold zeros there
 #pragma unroll
@@ -258,7 +255,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
             for (int ct = 0; ct < CT; ct++) s[ct][t] = (f4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < NK; k++) {
-                const bf8 kf = codes_to_bf16(kr[t][2 * k], kr[t][2 * k + 1]);
+                const bf8 kf = codes_to_bf16(kr[t][2 * k], kr[t][2 * k + 1], ksJ);
 #pragma unroll
                 for (int ct = 0; ct < CT; ct++)
 #pragma unroll

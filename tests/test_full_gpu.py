@@ -223,6 +223,111 @@ def test_attend_scales_far_apart():
         p.attend(q)
 
 
+@pytest.mark.parametrize("g,d", [(20, 64), (32, 128), (17, 32), (16, 256), (17, 256)])
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f32", "f32")])
+def test_steps_of_wide_groups(g, d, dtype, out):
+    """Generation steps with 16 to 32 query heads per kv head (two column tiles; at d = 256 the prompt kernel from 17 on), a block filling up."""
+    rng = np.random.default_rng(g + d)
+    p = Pair(1, 2 * g, 2, d, 640, dtype, out)
+    p.append(*p.tokens(rng, 61)[1:])
+    for t in range(6):
+        p.step(*p.tokens(rng, 1, 0.5 * 2 ** t), gather=t % 2 == 1)     # (growing magnitudes: the block is rescaled in the step)
+        p.check_memory(weights=False)
+
+
+def test_step_of_many_streams():
+    """More streams than compute units: one workgroup of eight wavefronts each, caches beyond 512 slots."""
+    rng = np.random.default_rng(77)
+    p = Pair(65, 16, 4, 32, 1024, out="f32")
+    p.append(*p.tokens(rng, 700)[1:], [700 - 10 * b for b in range(65)])
+    p.step(*p.tokens(rng, 1))
+    p.step(*p.tokens(rng, 1), gather=True)
+    p.check_memory(weights=False)
+
+
+def test_single_tokens_with_lens():
+    """attend of one token where some sequences have none."""
+    rng = np.random.default_rng(78)
+    for cap in (128, 4096):
+        p = Pair(3, 8, 2, 64, cap)
+        p.append(*p.tokens(rng, 70)[1:])
+        q, k, v = p.tokens(rng, 1)
+        p.append(k, v, [1, 0, 1])
+        p.check_memory()
+        p.attend(q, [1, 0, 1], gather=True)
+
+
+def test_step_on_a_full_cache():
+    """The library stores what fits: the token of a full stream is counted and not stored, its query sees what is there."""
+    rng = np.random.default_rng(79)
+    for gather in (False, True):
+        p = Pair(2, 4, 1, 64, 128)
+        p.append(*p.tokens(rng, 128)[1:], [128, 100])
+        q, k, v = p.tokens(rng, 1)
+        before = p.c.weight.clone()
+        y = torch.empty((2, 4, 64), device=DEV)
+        ws = torch.empty(lb.lola_full_workspace_bytes(p.c.cfg, 1, True), dtype=torch.uint8, device=DEV)
+        lb.lola_full_step(p.c.cfg, p.c.st, *(x[:, :, 0].contiguous().to(DEV) for x in (q, k, v)), int(gather), y, ws)
+        p.o.append(k.double().numpy(), v.double().numpy())
+        before[1, 0, 100] = 0
+        p.check_memory(weights=False)
+        p.check_out(y[:, :, None], q, None, gather, before if gather else None)
+        with pytest.raises(lb.LolaError, match="evict"):
+            p.c.step(*(x[:, :, 0].contiguous().to(DEV) for x in (q, k, v)))
+
+
+def test_weights_beside_nan_tokens():
+    """Queries that see a NaN token add no weight; those before it do."""
+    rng = np.random.default_rng(80)
+    for T in (6, 100):
+        p = Pair(1, 4, 1, 64, 256)
+        q, k, v = p.tokens(rng, T)
+        k[0, 0, T // 2, 3] = float("nan")
+        p.append(k, v)
+        p.attend(q, gather=True)
+
+
+def test_large_fp32_queries():
+    """fp32 queries up to the largest finite number enter the products unchanged (tiny keys keep the logits finite)."""
+    rng = np.random.default_rng(81)
+    for T in (1, 40):
+        p = Pair(1, 4, 1, 64, 128, "f32")
+        q, k, v = p.tokens(rng, T)
+        q = torch.sign(q) * 3.4e38
+        p.append(k * 2.0 ** -100, v)
+        p.c.cfg.softmax_scale = p.o.scale = 2.0 ** -28
+        p.attend(q)
+
+
+def test_captured_calls_and_the_bound_on_the_host():
+    """Replays are not seen by the host: calls outside the graph look at the counts; a workspace that a graph uses outlives a larger one."""
+    rng = np.random.default_rng(82)
+    c = lb.LolaFullCache(1, 4, 1, 64, 256, device=DEV)
+    tok = [x.to(DEV) for x in (rng_tokens(rng, (1, 4, 64), "bf16")[0], rng_tokens(rng, (1, 1, 64), "bf16")[0], rng_tokens(rng, (1, 1, 64), "bf16")[0])]
+    c.step(*tok)
+    out = torch.empty((1, 4, 64), device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.step(*tok, out=out, gather=True)
+    used = c.workspace
+    for _ in range(250):
+        graph.replay()
+    assert int(c.count.max()) == 251
+    kv = tok[1][:, :, None].expand(1, 1, 6, 64).contiguous()
+    with pytest.raises(lb.LolaError, match="evict"):
+        c.append(kv, kv)
+    c.append(kv[:, :, :5].contiguous(), kv[:, :, :5].contiguous())
+    q = tok[0][:, :, None].expand(1, 4, 200, 64).contiguous()
+    c.attend(q, gather=True)
+    assert c.workspace is used or any(w is used for w in c._outgrown)
+    graph.replay()      # full: the token is not stored
+    torch.cuda.synchronize()
+    assert int(c.count.max()) == 256 and int(c.n_tokens.max()) == 257
+    c.evict(10)
+    c.append(kv, kv)
+    assert int(c.count.max()) == 16
+
+
 @pytest.mark.parametrize("d", [32, 64, 128, 256])
 @pytest.mark.parametrize("n,keep,first,recent", [(200, 64, 0, 0), (200, 100, 4, 10), (130, 129, 0, 1), (300, 1, 0, 0), (300, 0, 0, 0), (257, 192, 3, 0),
                                                  (64, 64, 0, 0), (640, 77, 40, 37), (640, 600, 0, 16)])
