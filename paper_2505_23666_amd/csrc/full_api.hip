@@ -338,19 +338,22 @@ lola_status lola_full_evict(const lola_full_config *c, const lola_full_state *st
     a.edge = (float *)(ws + p.off_edge);
     a.most = p.most; a.nkb = p.nkb;
     const int S = c->batch * c->n_kv_heads;
-    // (up to 8192 slots in workgroups of 256, of which more fit a compute unit)
     const int lds = a.cap <= RANKS_LDS ? a.cap * 4 : 0;
+#define BY_DIM(K) (a.d == 32 ? K<32> : a.d == 64 ? K<64> : a.d == 128 ? K<128> : K<256>)
+    // Short caches from which at most 512 pairs can move: the whole eviction of a stream in one workgroup (with the append of a
+    // turn, 16 sequences of the 8B shape with a budget of 2048 pairs 22.7 us, 24.5 by the kernels below; 128 of the 1B shape with 1111 23.8 and 28.8).
+    if (a.cap <= 8192 && a.most <= 512) {
+        hipLaunchKernelGGL(BY_DIM(evict_few_kernel), dim3(S), dim3(256), lds + (2 * a.most + 3 * a.nkb) * 4, (hipStream_t)stream, a);
+        LAUNCH_CHECK();
+        return LOLA_OK;
+    }
+    // (up to 8192 slots in workgroups of 256, of which more fit a compute unit)
     if (a.cap <= 8192) hipLaunchKernelGGL((evict_select_kernel<256>), dim3(S), dim3(256), lds, (hipStream_t)stream, a);
     else hipLaunchKernelGGL((evict_select_kernel<1024>), dim3(S), dim3(1024), lds, (hipStream_t)stream, a);
     LAUNCH_CHECK();
     if (p.nkb == 0) return LOLA_OK;
-    // Up to eight pairs a block on average: one wavefront per block (128 sequences of the 1B shape back to 1111 pairs after 16 tokens 18 us with
-    // four); beyond, four (32 Ki pairs cut to 2048).
-    const bool few = p.most <= 8 * p.nkb;
-    const dim3 grid(few ? (p.nkb + 3) / 4 : p.nkb, S);
-#define MOVE(DH) (few ? evict_move_kernel<DH, 1> : evict_move_kernel<DH, 4>)
-    hipLaunchKernelGGL((a.d == 32 ? MOVE(32) : a.d == 64 ? MOVE(64) : a.d == 128 ? MOVE(128) : MOVE(256)), grid, dim3(256), 0, (hipStream_t)stream, a);
-#undef MOVE
+    hipLaunchKernelGGL(BY_DIM(evict_move_kernel), dim3(p.nkb, S), dim3(256), 0, (hipStream_t)stream, a);
+#undef BY_DIM
     LAUNCH_CHECK();
     return LOLA_OK;
 }

@@ -228,26 +228,17 @@ __device__ __forceinline__ int scan_all(int v, int *wsum, int *total) {
 
 constexpr int RANKS_LDS = 32768;   // ranks that the selection keeps in LDS; longer caches compute them again in each pass
 
-// One workgroup per stream finds the keep-th largest rank in three passes over the ranks (11, 11 and 10 bits: a histogram in LDS
-// and a scan over its bins), then writes the lists.  A thread takes four slots at a time.  Bound by latency: a handful of dependent passes
-// over a few thousand ranks.
+constexpr int RANK_BINS = 2048;
+struct SelectLds { int hist[RANK_BINS], wsum[16], found[3]; };
+
+// The workgroup finds the stream's keep-th largest rank (0 < keep < count) in three passes over the ranks (11, 11 and 10 bits: a histogram in LDS
+// and a scan over its bins), then writes the lists: dst, src, and before (may be NULL) without its last entry.  A thread takes four
+// slots at a time.  Returns the number of pairs that move.
 template <int NT>
-__global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
-    constexpr int NB = 2048, BPT = NB / NT;
-    extern __shared__ __attribute__((aligned(16))) uint32_t rank_l[];     // [min(cap, RANKS_LDS)] where they fit
-    __shared__ int hist[NB], wsum[NT / 64], found[3];
-    const int si = blockIdx.x, tid = threadIdx.x;
-    int count = a.mem.count[si];
-    count = count < 0 ? 0 : (count > a.cap ? a.cap : count);
-    int32_t *before = a.before + (size_t)si * (a.nkb + 1);
-    if (count <= a.keep) {
-        for (int J = tid; J <= a.nkb; J += NT) before[J] = 0;
-        return;
-    }
-    if (a.keep == 0) {      // nothing to rank
-        if (tid == 0) a.mem.count[si] = 0;
-        return;
-    }
+__device__ __forceinline__ int select_pairs(const EvictArgs &a, int si, int count, uint32_t *rank_l, SelectLds &l, int32_t *dst, int32_t *src, int32_t *before) {
+    constexpr int NB = RANK_BINS, BPT = NB / NT;
+    int *hist = l.hist, *wsum = l.wsum, *found = l.found;
+    const int tid = threadIdx.x;
     const size_t base = (size_t)si * a.cap;
     const int64_t recent_from = a.mem.n_tokens[si] - a.recent;
     const bool cached = a.cap <= RANKS_LDS;
@@ -322,14 +313,36 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
         int all;
         const int at = scan_all<NT>(kinds, wsum, &all);
         int h_at = holes + (at & 0xFFFF), m_at = moved + (at >> 16);
-        if (s % BLK == 0 && s < a.keep) before[s / BLK] = h_at;
+        if (before && s % BLK == 0 && s < a.keep) before[s / BLK] = h_at;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            if (hole[e] && h_at < a.most) a.dst[(size_t)si * a.most + h_at++] = s + e;
-            if (mover[e] && m_at < a.most) a.src[(size_t)si * a.most + m_at++] = s + e;
+            if (hole[e] && h_at < a.most) dst[h_at++] = s + e;
+            if (mover[e] && m_at < a.most) src[m_at++] = s + e;
         }
         holes += all & 0xFFFF; moved += all >> 16;
     }
+    return holes;
+}
+
+// One workgroup per stream: the lists of evict_move_kernel.  Bound by latency: a handful of dependent passes over a few thousand ranks
+// (12 us for 2112 of 2048 pairs of 128 streams).
+template <int NT>
+__global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint32_t rank_l[];     // [min(cap, RANKS_LDS)] where they fit
+    __shared__ SelectLds l;
+    const int si = blockIdx.x, tid = threadIdx.x;
+    int count = a.mem.count[si];
+    count = count < 0 ? 0 : (count > a.cap ? a.cap : count);
+    int32_t *before = a.before + (size_t)si * (a.nkb + 1);
+    if (count <= a.keep) {
+        for (int J = tid; J <= a.nkb; J += NT) before[J] = 0;
+        return;
+    }
+    if (a.keep == 0) {      // nothing to rank
+        if (tid == 0) a.mem.count[si] = 0;
+        return;
+    }
+    const int holes = select_pairs<NT>(a, si, count, rank_l, l, a.dst + (size_t)si * a.most, a.src + (size_t)si * a.most, before);
     if (tid == 0) {
         before[a.nkb] = holes;
         if (a.keep % BLK) {
@@ -340,17 +353,110 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
     }
 }
 
+// The whole eviction of a stream by one workgroup, where few pairs can move: the lists stay in LDS, the pairs are moved side by side rather
+// than block by block.  Each pair raises its block's exponents to what it needs (an LDS maximum), blocks whose exponent grew are
+// rescaled, then the pairs are written; the scales themselves last, since a pair may come from the block that the budget ends in.
+template <int DH>
+__global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
+    constexpr int TPR = DH / 8, RPP = 256 / TPR, U = 4;      // threads per row, rows per pass, passes held in registers
+    extern __shared__ __attribute__((aligned(16))) uint32_t rank_l[];     // ranks [cap], then dst, src [most], exponents of keys, values [nkb], grown [nkb]
+    __shared__ SelectLds l;
+    __shared__ int ngrown;
+    const int si = blockIdx.x, tid = threadIdx.x;
+    int count = a.mem.count[si];
+    count = count < 0 ? 0 : (count > a.cap ? a.cap : count);
+    if (count <= a.keep) return;
+    if (a.keep == 0) {
+        if (tid == 0) a.mem.count[si] = 0;
+        return;
+    }
+    int *dst = (int *)rank_l + a.cap, *src = dst + a.most, *ek = src + a.most, *ev = ek + a.nkb, *grown = ev + a.nkb;
+    float *ks = a.mem.ks + (size_t)si * a.nblk, *vs = a.mem.vs + (size_t)si * a.nblk;
+    for (int J = tid; J < a.nkb; J += 256) { ek[J] = exponent_of(ks[J]); ev[J] = exponent_of(vs[J]); }
+    if (tid == 0) ngrown = 0;
+    const int n = select_pairs<256>(a, si, count, rank_l, l, dst, src, nullptr);
+    __syncthreads();
+    const size_t base = (size_t)si * a.cap;
+    const int col = (tid % TPR) * 8;
+    uint2 kc[U], vc[U];
+    float sk[U], sv[U];
+    auto load = [&](int p0) {
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int p = p0 + u * RPP + tid / TPR;
+            kc[u] = vc[u] = make_uint2(0, 0); sk[u] = sv[u] = 0.f;
+            if (p >= n) continue;
+            const int s = src[p];
+            kc[u] = *reinterpret_cast<const uint2 *>(a.mem.k + (base + s) * DH + col);
+            vc[u] = *reinterpret_cast<const uint2 *>(a.mem.v + (base + s) * DH + col);
+            sk[u] = ks[s / BLK]; sv[u] = vs[s / BLK];
+        }
+    };
+    for (int p0 = 0; p0 < n; p0 += U * RPP) {
+        load(p0);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int p = p0 + u * RPP + tid / TPR;
+            float x[8], mk = 0.f, mv = 0.f;
+            from_codes(kc[u].x, x); from_codes(kc[u].y, x + 4);
+#pragma unroll
+            for (int e = 0; e < 8; e++) mk = fmaxf(mk, fabsf(x[e]));   // (a NaN key counts as zero)
+            from_codes(vc[u].x, x); from_codes(vc[u].y, x + 4);
+#pragma unroll
+            for (int e = 0; e < 8; e++) mv = fmaxf(mv, fabsf(x[e]));
+#pragma unroll
+            for (int o = 1; o < TPR; o <<= 1) { mk = fmaxf(mk, __shfl_xor(mk, o)); mv = fmaxf(mv, __shfl_xor(mv, o)); }
+            if (p < n && tid % TPR == 0) {
+                atomicMax(&ek[dst[p] / BLK], fit_exponent(mk * sk[u]));
+                atomicMax(&ev[dst[p] / BLK], fit_exponent(mv * sv[u]));
+            }
+        }
+    }
+    __syncthreads();
+    for (int J = tid; J < a.nkb; J += 256)
+        if (ek[J] > exponent_of(ks[J]) || ev[J] > exponent_of(vs[J])) grown[atomicAdd(&ngrown, 1)] = J;
+    __syncthreads();
+    for (int i = 0; i < ngrown; i++) {
+        const int J = grown[i], dk = exponent_of(ks[J]) - ek[J], dv = exponent_of(vs[J]) - ev[J], rows = min(BLK, a.keep - J * BLK);
+        const float fk = pow2(max(dk, -40)), fv = pow2(max(dv, -40));
+        uint8_t *kb = a.mem.k + (base + (size_t)J * BLK) * DH, *vb = a.mem.v + (base + (size_t)J * BLK) * DH;
+        for (int e = tid; e < rows * TPR; e += 256) {
+            if (dk < 0) { uint2 u = reinterpret_cast<uint2 *>(kb)[e]; u.x = rescale_codes(u.x, fk); u.y = rescale_codes(u.y, fk); reinterpret_cast<uint2 *>(kb)[e] = u; }
+            if (dv < 0) { uint2 u = reinterpret_cast<uint2 *>(vb)[e]; u.x = rescale_codes(u.x, fv); u.y = rescale_codes(u.y, fv); reinterpret_cast<uint2 *>(vb)[e] = u; }
+        }
+    }
+    if (ngrown) __syncthreads();      // (rows that moved pairs replace were rescaled by other threads)
+    for (int p0 = 0; p0 < n; p0 += U * RPP) {
+        if (n > U * RPP) load(p0);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int p = p0 + u * RPP + tid / TPR;
+            if (p >= n) continue;
+            const int t = dst[p], J = t / BLK, s = src[p];
+            const float fk = pow2(min(40, max(exponent_of(sk[u]) - ek[J], -40))), fv = pow2(min(40, max(exponent_of(sv[u]) - ev[J], -40)));
+            uint2 c = kc[u];
+            c.x = rescale_codes(c.x, fk); c.y = rescale_codes(c.y, fk);
+            *reinterpret_cast<uint2 *>(a.mem.k + (base + t) * DH + col) = c;
+            c = vc[u];
+            c.x = rescale_codes(c.x, fv); c.y = rescale_codes(c.y, fv);
+            *reinterpret_cast<uint2 *>(a.mem.v + (base + t) * DH + col) = c;
+            if (tid % TPR == 0) { a.mem.idx[base + t] = a.mem.idx[base + s]; a.mem.weight[base + t] = a.mem.weight[base + s]; }
+        }
+    }
+    __syncthreads();      // every source's scale has been read
+    for (int i = tid; i < ngrown; i += 256) { const int J = grown[i]; ks[J] = pow2(ek[J]); vs[J] = pow2(ev[J]); }
+    if (tid == 0) a.mem.count[si] = a.keep;
+}
+
 // The pairs that move into a block below the budget come from slots at and beyond `keep`, which no workgroup writes.  (Of the block
 // that the budget ends in only rows below it are rescaled; its scales, which others read as a source's, are read from the copy
-// taken beforehand.)  WPB wavefronts take a block: four where many pairs move, one (four blocks per workgroup) where few do.  Up to four
-// passes over the rows are held in registers between finding the exponent and writing.
-template <int DH, int WPB>
+// taken beforehand.)  One workgroup per block; up to four passes over the rows are held in registers between finding the exponent
+// and writing.
+template <int DH>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
-    constexpr int TPR = DH / 8, RPP = 64 * WPB / TPR, U = 4;      // threads per row, rows per pass, passes held
+    constexpr int TPR = DH / 8, RPP = 256 / TPR, U = 4;      // threads per row, rows per pass, passes held
     __shared__ float red[2][4];
-    const int si = blockIdx.y, w = threadIdx.x >> 6, lane = threadIdx.x & 63, tid = WPB == 4 ? threadIdx.x : lane;
-    const int J = WPB == 4 ? blockIdx.x : blockIdx.x * 4 + w;
-    if (J >= a.nkb) return;      // (with one wavefront per block there is no workgroup barrier)
+    const int si = blockIdx.y, w = threadIdx.x >> 6, lane = threadIdx.x & 63, tid = threadIdx.x, J = blockIdx.x;
     const int j0 = a.before[(size_t)si * (a.nkb + 1) + J], j1 = a.before[(size_t)si * (a.nkb + 1) + J + 1];
     if (j0 >= j1) return;
     const int32_t *dst = a.dst + (size_t)si * a.most, *src = a.src + (size_t)si * a.most;
@@ -396,24 +502,21 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
         }
     }
     ak = wave_max(ak); av = wave_max(av);
-    if (WPB == 4) {
-        if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
-        __syncthreads();
-        ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-        av = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
-    }
+    if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
+    __syncthreads();
+    ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    av = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
     const int ok = exponent_of(ok_s), ov = exponent_of(ov_s), ek = max(ok, fit_exponent(ak)), ev = max(ov, fit_exponent(av));
     uint8_t *kb = a.mem.k + (base + (size_t)J * BLK) * DH, *vb = a.mem.v + (base + (size_t)J * BLK) * DH;
     if (ek > ok || ev > ov) {
         const float fk = pow2(max(ok - ek, -40)), fv = pow2(max(ov - ev, -40));
         const int rows = min(BLK, a.keep - J * BLK);
-        for (int e = tid; e < rows * TPR; e += 64 * WPB) {
+        for (int e = tid; e < rows * TPR; e += 256) {
             if (ek > ok) { uint2 u = reinterpret_cast<uint2 *>(kb)[e]; u.x = rescale_codes(u.x, fk); u.y = rescale_codes(u.y, fk); reinterpret_cast<uint2 *>(kb)[e] = u; }
             if (ev > ov) { uint2 u = reinterpret_cast<uint2 *>(vb)[e]; u.x = rescale_codes(u.x, fv); u.y = rescale_codes(u.y, fv); reinterpret_cast<uint2 *>(vb)[e] = u; }
         }
         if (tid == 0) { a.mem.ks[(size_t)si * a.nblk + J] = pow2(ek); a.mem.vs[(size_t)si * a.nblk + J] = pow2(ev); }
-        // the rows that the moved pairs replace were rescaled by other threads
-        if (WPB == 4) __syncthreads(); else __threadfence_block();
+        __syncthreads();   // the rows that the moved pairs replace were rescaled by other threads
     }
     for (int jb = j0; jb < j1; jb += U * RPP) {
         if (j1 - j0 > U * RPP) load(jb);

@@ -358,6 +358,26 @@ def test_evict(d, n, keep, first, recent):
     p.attend(q)
 
 
+@pytest.mark.parametrize("d,cap,n,keep", [(32, 2048, 2000, 1000), (64, 2048, 1900, 777), (128, 1344, 1344, 640), (256, 1280, 1280, 601), (64, 10240, 9000, 1000),
+                                          (32, 36864, 35000, 3000)])
+def test_evict_from_longer_caches(d, cap, n, keep):
+    """Many pairs move, blocks of very different scales among them."""
+    rng = np.random.default_rng(cap + d)
+    p = Pair(1, 2, 2, d, cap)
+    _, k, v = p.tokens(rng, n)
+    k, v = (x * torch.from_numpy(np.ldexp(1.0, rng.integers(-9, 10, (1, 2, n, 1)))).to(x.dtype) for x in (k, v))
+    p.append(k, v)
+    w = rng.integers(0, 400, (1, 2, cap)).astype(np.float32) / 64
+    w[rng.random(w.shape) < 0.01] = np.nan
+    p.c.weight.copy_(torch.from_numpy(w))
+    for b, h, s in p.o.each():
+        s.weight[:] = w[b, h]
+    for to in (keep, keep - keep // 3):
+        p.c.evict(to, 4, 50)
+        p.o.evict(to, 4, 50)
+        p.check_memory()
+
+
 def test_evict_many_pairs_and_streams():
     """Distinct weights over several thousand slots: ranks that differ in their lowest bits alone."""
     rng = np.random.default_rng(3)
