@@ -182,6 +182,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         J = next(J0);
     }
     const float c = a.scale2;
+    const float minus_one = opaque_minus_one();
     float vref = 0.f, vstage = 0.f;      // o is in units of vref; the staged block's values in units of vstage
     bool masked = false;
     if (J < J1) {
@@ -248,12 +249,13 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off));
-                sum += p;
-                const _Float16 ph = (_Float16)p;
-                pf[kt * 2 + e / 8][0][e & 7] = ph;
-                if (PP == 2) pf[kt * 2 + e / 8][PP - 1][e & 7] = (_Float16)(p - (float)ph);
+            for (int e = 0; e < 16; e += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), y = __builtin_amdgcn_exp2f(fmaf(s[kt][e + 1], c, -off));
+                sum += x; sum += y;
+                h2 part[PP];
+                to_f16_parts<PP>(x, y, minus_one, part);
+#pragma unroll
+                for (int p = 0; p < PP; p++) { pf[kt * 2 + e / 8][p][e & 7] = part[p][0]; pf[kt * 2 + e / 8][p][(e & 7) + 1] = part[p][1]; }
             }
         l += sum;
 #pragma unroll
@@ -335,6 +337,20 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs pa) {
 #pragma unroll
     for (int e = 0; e < 4; e++) stf(op, col + e, L == 0.f ? 0.f : acc[e] / L);
     if (pa.stat && col == 0) pa.stat[(size_t)si * R + r] = (L > 0.f && finite(L)) ? mu + __builtin_amdgcn_logf(L) - SHIFT : INFINITY;
+}
+
+// sum over the 32 lanes of a half wavefront, in each of them: lane permutations within rows of 16, then a row swap
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+    return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float sum32(float v) {
+    v = add_dpp<0xB1>(v);        // lane ^ 1
+    v = add_dpp<0x4E>(v);        // lane ^ 2
+    v = add_dpp<0x141>(v);       // 7 - lane of each eight
+    v = add_dpp<0x140>(v);       // 15 - lane of each sixteen
+    const Two t = swap_rows16(v);
+    return t.a + t.b;
 }
 
 // weight[j] += sum over rows of 2^(logit - stat): one workgroup per block of slots, whose keys stay in registers as the first operand of
@@ -426,8 +442,7 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
 #pragma unroll
             for (int e = 0; e < 16; e++) {
                 float v = acc[kt][e];
-#pragma unroll
-                for (int x = 1; x < 32; x <<= 1) v += __shfl_xor(v, x);
+                v = sum32(v);
                 if (l32 == 0) sum_l[w][kt * 32 + (e / 4) * 8 + hi * 4 + (e & 3)] = v;
             }
         __syncthreads();

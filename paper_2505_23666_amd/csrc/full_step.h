@@ -60,6 +60,24 @@ __device__ __forceinline__ void split_bf16(const float *x, bf8 *part) {
     }
 }
 
+// Two fp32 numbers as fp16 operand parts: rounded, and (where PP = 2) what the rounding left, rounded.  The difference is one mixed-precision
+// fused operation per number; minus_one holds -1 where the compiler cannot see it (it would make a conversion and a subtraction).
+template <int PP>
+__device__ __forceinline__ void to_f16_parts(float x, float y, float minus_one, h2 *part) {
+    part[0] = (h2){(_Float16)x, (_Float16)y};
+    if (PP == 2) {      // (one packed conversion whose halves are read again, not two more)
+        uint32_t u = __builtin_bit_cast(uint32_t, part[0]);
+        asm("" : "+v"(u));
+        part[0] = __builtin_bit_cast(h2, u);
+    }
+    if (PP == 2) part[PP - 1] = (h2){(_Float16)__builtin_fmaf((float)part[0][0], minus_one, x), (_Float16)__builtin_fmaf((float)part[0][1], minus_one, y)};
+}
+__device__ __forceinline__ float opaque_minus_one() {
+    float x = -1.f;
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 struct StepArgs {
     Args a;
     int nsplit;
@@ -234,6 +252,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
         for (int c = 0; c < ND; c++) o[ct][c] = (f4){0.f, 0.f, 0.f, 0.f};
     }
     uint8_t *st = stage[w];
+    const float minus_one = opaque_minus_one();
     for (int J = J0 + w, it = 0; J < J1; J += NW, it++) {
         if (it == 64) { it = 0; scales(J); }
         const float ksJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksT), it)), vsJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsT), it));
@@ -291,12 +310,13 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
 #pragma unroll
             for (int t = 0; t < 4; t++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const float p = __builtin_amdgcn_exp2f(s[ct][t][e] - (mu - P_SHIFT));
-                    sum += p;
-                    const _Float16 hi = (_Float16)p;
-                    pf[ct][t / 2][0][(t & 1) * 4 + e] = hi;
-                    if (PP == 2) pf[ct][t / 2][PP - 1][(t & 1) * 4 + e] = (_Float16)(p - (float)hi);
+                for (int e = 0; e < 4; e += 2) {
+                    const float x = __builtin_amdgcn_exp2f(s[ct][t][e] - (mu - P_SHIFT)), y = __builtin_amdgcn_exp2f(s[ct][t][e + 1] - (mu - P_SHIFT));
+                    sum += x + y;
+                    h2 part[PP];
+                    to_f16_parts<PP>(x, y, minus_one, part);
+#pragma unroll
+                    for (int p = 0; p < PP; p++) { pf[ct][t / 2][p][(t & 1) * 4 + e] = part[p][0]; pf[ct][t / 2][p][(t & 1) * 4 + e + 1] = part[p][1]; }
                 }
             l[ct] = l[ct] * f + quad_sum(sum);
 #pragma unroll
