@@ -1,6 +1,7 @@
 /*
  * lola.h - C ABI of the MI355X (gfx950) implementation of one LoLA attention layer
- * (LoLA: Low-Rank Linear Attention with Sparse Caching, arxiv 2505.23666).
+ * (LoLA: Low-Rank Linear Attention with Sparse Caching, arxiv 2505.23666), and, at its end, of softmax attention over an 8-bit
+ * full-context cache (lola_full_*).
  *
  * The library owns no memory and never synchronises: every pointer below is a DEVICE pointer
  * (unless marked host) to caller-owned, contiguous, row-major memory aligned to 16 bytes, and

@@ -9,6 +9,11 @@
 // transposing 16-bit LDS read.  Which blocks can be passed over and which need a comparison per element follows from the least and largest token
 // index of each block (of long caches taken beforehand by a kernel of its own): slots need not be in the order of tokens (evictions fill holes).
 //
+// Bound by the sum of its matrix and vector instructions, of two wavefronts per SIMD, and by power: four prompts of 4096 tokens (32 query, 8 kv
+// heads, d = 128, bf16) 0.59 ms alone, 930 TFLOP/s, where a large library product reaches 1330; the same with all elements equal is a fifth
+// faster.  A block of a wavefront is 32 products of 32 cycles, 32 exponentials, about 200 other vector instructions and 32 KB from LDS.  At
+// d = 64 the exponentials weigh as much as the products (two prompts of 2000 tokens, fp32 outputs: 72 us).
+//
 // The maximum is only moved when a logit exceeds it by more than 2^RAISE: weights then reach 2^RAISE, held times 2^SHIFT in fp16.
 #pragma once
 #include <type_traits>
@@ -354,7 +359,8 @@ __device__ __forceinline__ float sum32(float v) {
 }
 
 // weight[j] += sum over rows of 2^(logit - stat): one workgroup per block of slots, whose keys stay in registers as the first operand of
-// S^T = K Q^T; the wavefronts take 32 rows in turn, straight from global memory, and join their sums at the end
+// S^T = K Q^T; the wavefronts take 32 rows in turn, straight from global memory, and join their sums at the end.  Bound by vector
+// instructions: an exponential and three others per logit (two prompts of 2000 tokens at d = 64: 57 us, 16.4 GFLOP).
 template <int DH, typename TI>
 __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void prompt_gather_kernel(PromptArgs pa) {
     constexpr int QP = sizeof(TI) == 4 ? 3 : 1, NK = DH / 16;
