@@ -326,7 +326,7 @@ __device__ __forceinline__ int select_pairs(const EvictArgs &a, int si, int coun
 }
 
 // One workgroup per stream: the lists of evict_move_kernel.  Bound by latency: a handful of dependent passes over a few thousand ranks
-// (12 us for 2112 of 2048 pairs of 128 streams).
+// (32 Ki slots of 32 streams 31 us).
 template <int NT>
 __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint32_t rank_l[];     // [min(cap, RANKS_LDS)] where they fit
