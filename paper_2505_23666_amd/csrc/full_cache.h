@@ -64,6 +64,45 @@ __device__ __forceinline__ uint32_t rescale_codes(uint32_t c, float f) {
     return to_codes(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
 }
 
+// this lane's value and that of the lane 16 / 32 away (row swaps, no LDS round trip)
+struct Two { float a, b; };
+__device__ __forceinline__ Two swap_rows16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Two swap_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+
+// Permutations of lanes inside rows of 16, a vector instruction each (a shuffle goes through LDS, some 100 cycles)
+enum { PERM_XOR1 = 0xB1, PERM_XOR2 = 0x4E, PERM_MIRROR8 = 0x141, PERM_MIRROR16 = 0x140 };
+template <int PERM>
+__device__ __forceinline__ float lane_perm(float v) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), PERM, 0xF, 0xF, true));
+}
+// maximum over N neighbouring lanes (N = 4, 8, 16, 32, aligned), in each of them
+template <int N>
+__device__ __forceinline__ float max_of(float v) {
+    v = fmaxf(v, lane_perm<PERM_XOR1>(v));
+    v = fmaxf(v, lane_perm<PERM_XOR2>(v));
+    if (N >= 8) v = fmaxf(v, lane_perm<PERM_MIRROR8>(v));
+    if (N >= 16) v = fmaxf(v, lane_perm<PERM_MIRROR16>(v));
+    if (N >= 32) { const Two t = swap_rows16(v); v = fmaxf(t.a, t.b); }
+    return v;
+}
+__device__ __forceinline__ float max_of_wave(float v) { const Two t = swap_halves(max_of<32>(v)); return fmaxf(t.a, t.b); }
+// sums of the lanes up to and with this one
+__device__ __forceinline__ int scan_wave(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);     // from 1, 2, 4, 8 lanes below in the row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);     // the last lane of rows 0 and 2 to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);     // lane 31 to rows 2 and 3
+    return x;
+}
+
 __device__ __forceinline__ void load8(const float *p, float *x) {
     const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
@@ -125,14 +164,12 @@ __global__ __launch_bounds__(256) void append_kernel(Args a, int per, int advanc
                 if (!finite(y[p][e])) { nf = 1; y[p][e] = 0.f; }
                 av = fmaxf(av, fabsf(y[p][e]));
             }
-#pragma unroll
-            for (int o = 1; o < TPR; o <<= 1) nf |= __shfl_xor(nf, o);
-            bad[p] = nf != 0;
+            bad[p] = ((__ballot(nf) >> (lane & ~(TPR - 1))) & ((1ull << TPR) - 1)) != 0;     // any of the row's threads
             if (!bad[p])
 #pragma unroll
                 for (int e = 0; e < 8; e++) ak = fmaxf(ak, fabsf(x[p][e]));
         }
-        ak = wave_max(ak); av = wave_max(av);
+        ak = max_of_wave(ak); av = max_of_wave(av);
         __syncthreads();   // (the last block's readers are done)
         if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
         __syncthreads();
@@ -214,9 +251,7 @@ __device__ __forceinline__ uint32_t rank_of(int i, float w, int first, int64_t r
 template <int NT>
 __device__ __forceinline__ int scan_all(int v, int *wsum, int *total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    int x = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o); if (lane >= o) x += y; }
+    const int x = scan_wave(v);
     __syncthreads();
     if (lane == 63) wsum[w] = x;
     __syncthreads();
@@ -406,8 +441,7 @@ __global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
             from_codes(vc[u].x, x); from_codes(vc[u].y, x + 4);
 #pragma unroll
             for (int e = 0; e < 8; e++) mv = fmaxf(mv, fabsf(x[e]));
-#pragma unroll
-            for (int o = 1; o < TPR; o <<= 1) { mk = fmaxf(mk, __shfl_xor(mk, o)); mv = fmaxf(mv, __shfl_xor(mv, o)); }
+            mk = max_of<TPR>(mk); mv = max_of<TPR>(mv);
             if (p < n && tid % TPR == 0) {
                 atomicMax(&ek[dst[p] / BLK], fit_exponent(mk * sk[u]));
                 atomicMax(&ev[dst[p] / BLK], fit_exponent(mv * sv[u]));
@@ -503,7 +537,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
             av = fmaxf(av, mv * sv[u]);
         }
     }
-    ak = wave_max(ak); av = wave_max(av);
+    ak = max_of_wave(ak); av = max_of_wave(av);
     if (lane == 0) { red[0][w] = ak; red[1][w] = av; }
     __syncthreads();
     ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));

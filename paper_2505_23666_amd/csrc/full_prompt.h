@@ -344,16 +344,9 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs pa) {
     if (pa.stat && col == 0) pa.stat[(size_t)si * R + r] = (L > 0.f && finite(L)) ? mu + __builtin_amdgcn_logf(L) - SHIFT : INFINITY;
 }
 
-// sum over the 32 lanes of a half wavefront, in each of them: lane permutations within rows of 16, then a row swap
-template <int CTRL>
-__device__ __forceinline__ float add_dpp(float v) {
-    return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), CTRL, 0xF, 0xF, true));
-}
+// sum over the 32 lanes of a half wavefront, in each of them
 __device__ __forceinline__ float sum32(float v) {
-    v = add_dpp<0xB1>(v);        // lane ^ 1
-    v = add_dpp<0x4E>(v);        // lane ^ 2
-    v = add_dpp<0x141>(v);       // 7 - lane of each eight
-    v = add_dpp<0x140>(v);       // 15 - lane of each sixteen
+    v += lane_perm<PERM_XOR1>(v); v += lane_perm<PERM_XOR2>(v); v += lane_perm<PERM_MIRROR8>(v); v += lane_perm<PERM_MIRROR16>(v);
     const Two t = swap_rows16(v);
     return t.a + t.b;
 }

@@ -94,16 +94,6 @@ struct StepArgs {
 template <int DH>
 __device__ __forceinline__ int vswz(int row) { return (row / (256 / DH)) & (DH / 16 - 1); }
 
-// this lane's value and that of the lane 16 / 32 away (row swaps, no LDS round trip)
-struct Two { float a, b; };
-__device__ __forceinline__ Two swap_rows16(float v) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
-}
-__device__ __forceinline__ Two swap_halves(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
-}
 __device__ __forceinline__ float half_max(float v) { const Two t = swap_halves(v); return fmaxf(t.a, t.b); }
 __device__ __forceinline__ float half_sum(float v) { const Two t = swap_halves(v); return t.a + t.b; }
 __device__ __forceinline__ float quad_max(float v) { const Two t = swap_rows16(v); return half_max(fmaxf(t.a, t.b)); }
@@ -144,7 +134,7 @@ __device__ __forceinline__ void append_token(const Args &a, int si, int b, int h
         top = fmaxf(top, fabsf(x[e]));
     }
     const bool bad = __any(nf);
-    const float ak = bad ? 0.f : wave_max(isk ? top : 0.f), av = wave_max(isk ? 0.f : top);
+    const float ak = bad ? 0.f : max_of_wave(isk ? top : 0.f), av = max_of_wave(isk ? 0.f : top);
     int ek = fit_exponent(ak), ev = fit_exponent(av);
     uint8_t *kb = a.mem.k + ((size_t)si * a.cap + (size_t)J * BLK) * DH, *vb = a.mem.v + ((size_t)si * a.cap + (size_t)J * BLK) * DH;
     if (off > 0) {
