@@ -386,7 +386,7 @@ class LolaFullCache:
         if self.workspace is None or self.workspace.numel() < want:
             if self.workspace is not None:
                 self._outgrown.append(self.workspace)
-                want = max(want, 2 * self.workspace.numel())     # (all outgrown ones together are no larger than the last)
+                want = max(want, min(2 * self.workspace.numel(), self.workspace.numel() + (256 << 20)))     # (few of them)
             self.workspace = torch.empty(max(want, 16), dtype=torch.uint8, device=self.device)
         return self.workspace
 

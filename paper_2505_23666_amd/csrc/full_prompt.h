@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         spT = span[x]; ksT = ks[x]; vsT = vs[x];
         seen = __ballot(J + lane < J1 && (int64_t)spT.x <= wg_last);
     };
-    // the same from the indices themselves (short caches, up to 64 blocks: one launch less), a block per lane
+    // the same from the indices themselves (short caches, a block per lane: one launch less)
     auto table_of_indices = [&]() {
         base = J0;
         const int x = min(J0 + lane, a.nblk - 1), live = count - x * BLK;
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
             r += 128; t += t_step; hd += h_step;
             if (hd >= a.g) { hd -= a.g; t++; }
             load();
-            // fmaxf drops what rows without weight (off infinite) make of a NaN key
+            // a weight is in [0, 1]; the clamp, an output modifier of the exponential, makes 0 of what rows without weight (off infinite) make of a NaN key
             if (masked) {
 #pragma unroll
                 for (int kt = 0; kt < 2; kt++)
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) acc[kt][e] += fmaxf(__builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), 0.f);
+                for (int e = 0; e < 16; e++) acc[kt][e] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), 0.f, 1.f);
         }
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
