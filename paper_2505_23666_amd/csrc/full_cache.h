@@ -279,11 +279,12 @@ __device__ __forceinline__ int select_pairs(const EvictArgs &a, int si, int coun
     const int64_t recent_from = a.mem.n_tokens[si] - a.recent;
     const bool cached = a.cap <= RANKS_LDS;
     // ranks of slots s .. s + 3 (s a multiple of four; beyond count: nothing looks at them)
-    auto compute = [&](int s) {
-        const int4 i = *reinterpret_cast<const int4 *>(a.mem.idx + base + s);
-        const float4 w = *reinterpret_cast<const float4 *>(a.mem.weight + base + s);
+    auto ranks_of = [&](int4 i, float4 w) {
         return make_uint4(rank_of(i.x, w.x, a.first, recent_from), rank_of(i.y, w.y, a.first, recent_from),
                           rank_of(i.z, w.z, a.first, recent_from), rank_of(i.w, w.w, a.first, recent_from));
+    };
+    auto compute = [&](int s) {
+        return ranks_of(*reinterpret_cast<const int4 *>(a.mem.idx + base + s), *reinterpret_cast<const float4 *>(a.mem.weight + base + s));
     };
     auto ranks = [&](int s) { return cached ? *reinterpret_cast<const uint4 *>(rank_l + s) : compute(s); };
     uint32_t prefix = 0, mask = 0;
@@ -294,17 +295,32 @@ __device__ __forceinline__ int select_pairs(const EvictArgs &a, int si, int coun
         const uint32_t digit = pass == 2 ? 1023u : 2047u;
         for (int i = tid; i < NB; i += NT) hist[i] = 0;
         __syncthreads();
-        for (int s = tid * 4; s < count; s += NT * 4) {
-            uint4 u;
-            if (pass == 0) {
-                u = compute(s);
-                if (cached) *reinterpret_cast<uint4 *>(rank_l + s) = u;
-            } else u = ranks(s);
+        auto count_in = [&](int s, uint4 u) {
             const uint32_t us[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int e = 0; e < 4; e++)
                 if (s + e < count && (us[e] & mask) == prefix) atomicAdd(&hist[(us[e] >> shift) & digit], 1);
-        }
+        };
+        if (pass == 0) {      // (sixteen slots' loads under way at a time)
+            for (int s0 = tid * 4; s0 < count; s0 += NT * 16) {
+                int4 i[4];
+                float4 w[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const int s = s0 + x * NT * 4;
+                    if (s < count) { i[x] = *reinterpret_cast<const int4 *>(a.mem.idx + base + s); w[x] = *reinterpret_cast<const float4 *>(a.mem.weight + base + s); }
+                }
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const int s = s0 + x * NT * 4;
+                    if (s >= count) continue;
+                    const uint4 u = ranks_of(i[x], w[x]);
+                    if (cached) *reinterpret_cast<uint4 *>(rank_l + s) = u;
+                    count_in(s, u);
+                }
+            }
+        } else
+            for (int s = tid * 4; s < count; s += NT * 4) count_in(s, ranks(s));
         __syncthreads();
         // bins from the largest down: thread t has BPT of them from NB - 1 - t BPT on
         int mine = 0, total;
@@ -409,14 +425,16 @@ __global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
     }
     int *dst = (int *)rank_l + a.cap, *src = dst + a.most, *ek = src + a.most, *ev = ek + a.nkb, *grown = ev + a.nkb;
     float *ks = a.mem.ks + (size_t)si * a.nblk, *vs = a.mem.vs + (size_t)si * a.nblk;
-    for (int J = tid; J < a.nkb; J += 256) { ek[J] = exponent_of(ks[J]); ev[J] = exponent_of(vs[J]); }
+    int ok = 0, ov = 0;      // of block tid (at most 128 blocks)
+    if (tid < a.nkb) { ek[tid] = ok = exponent_of(ks[tid]); ev[tid] = ov = exponent_of(vs[tid]); }
     if (tid == 0) ngrown = 0;
     const int n = select_pairs<256>(a, si, count, rank_l, l, dst, src, nullptr);
     __syncthreads();
     const size_t base = (size_t)si * a.cap;
     const int col = (tid % TPR) * 8;
     uint2 kc[U], vc[U];
-    float sk[U], sv[U];
+    float sk[U], sv[U], wt[U];
+    int32_t id[U];
     auto load = [&](int p0) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
@@ -427,6 +445,7 @@ __global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
             kc[u] = *reinterpret_cast<const uint2 *>(a.mem.k + (base + s) * DH + col);
             vc[u] = *reinterpret_cast<const uint2 *>(a.mem.v + (base + s) * DH + col);
             sk[u] = ks[s / BLK]; sv[u] = vs[s / BLK];
+            id[u] = a.mem.idx[base + s]; wt[u] = a.mem.weight[base + s];
         }
     };
     for (int p0 = 0; p0 < n; p0 += U * RPP) {
@@ -449,8 +468,7 @@ __global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
         }
     }
     __syncthreads();
-    for (int J = tid; J < a.nkb; J += 256)
-        if (ek[J] > exponent_of(ks[J]) || ev[J] > exponent_of(vs[J])) grown[atomicAdd(&ngrown, 1)] = J;
+    if (tid < a.nkb && (ek[tid] > ok || ev[tid] > ov)) grown[atomicAdd(&ngrown, 1)] = tid;
     __syncthreads();
     for (int i = 0; i < ngrown; i++) {
         const int J = grown[i], dk = exponent_of(ks[J]) - ek[J], dv = exponent_of(vs[J]) - ev[J], rows = min(BLK, a.keep - J * BLK);
@@ -468,7 +486,7 @@ __global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
         for (int u = 0; u < U; u++) {
             const int p = p0 + u * RPP + tid / TPR;
             if (p >= n) continue;
-            const int t = dst[p], J = t / BLK, s = src[p];
+            const int t = dst[p], J = t / BLK;
             const float fk = pow2(min(40, max(exponent_of(sk[u]) - ek[J], -40))), fv = pow2(min(40, max(exponent_of(sv[u]) - ev[J], -40)));
             uint2 c = kc[u];
             c.x = rescale_codes(c.x, fk); c.y = rescale_codes(c.y, fk);
@@ -476,7 +494,7 @@ __global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
             c = vc[u];
             c.x = rescale_codes(c.x, fv); c.y = rescale_codes(c.y, fv);
             *reinterpret_cast<uint2 *>(a.mem.v + (base + t) * DH + col) = c;
-            if (tid % TPR == 0) { a.mem.idx[base + t] = a.mem.idx[base + s]; a.mem.weight[base + t] = a.mem.weight[base + s]; }
+            if (tid % TPR == 0) { a.mem.idx[base + t] = id[u]; a.mem.weight[base + t] = wt[u]; }
         }
     }
     __syncthreads();      // every source's scale has been read
