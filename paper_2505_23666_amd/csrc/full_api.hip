@@ -132,16 +132,24 @@ size_t evict_bytes(const lola_full_config *c) {
 
 template <typename TI>
 lola_status run_append(const Args &a, hipStream_t stream) {
-    // blocks that T tokens may fall into; a workgroup takes both of a short call's, so that it can move the counters on itself
-    // (grid y is limited to 65535)
-    const int w = (int)(((int64_t)a.T + 2 * BLK - 2) / BLK), per = w <= 2 ? w : (w + 32767) / 32768, adv = per == w;
+    // Blocks that T tokens may fall into.  One workgroup has all of a stream's, and moves the counters on itself, where they are at most two, or
+    // eight of short rows, four at a time (a prompt of 257 tokens, append and attention, 4 streams of 32 fp32 columns 20.5 us, 24.3 with a workgroup per
+    // block and a second launch; but 64 streams of 333 tokens of 128 bf16 columns 39.8 and 37.0).  (Grid y is limited to 65535.)
+    const int w = (int)(((int64_t)a.T + 2 * BLK - 2) / BLK);
+    const bool four = w > 2 && w <= 8 && a.d * sizeof(TI) <= 128;
+    const int per = w <= 2 || four ? w : (w + 32767) / 32768, adv = per == w;
     const dim3 grid(a.B * a.Hkv, (w + per - 1) / per);
-    switch (a.d) {
-        case 32: hipLaunchKernelGGL((append_kernel<32, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
-        case 64: hipLaunchKernelGGL((append_kernel<64, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
-        case 128: hipLaunchKernelGGL((append_kernel<128, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
-        default: hipLaunchKernelGGL((append_kernel<256, TI>), grid, dim3(256), 0, stream, a, per, adv); break;
+#define APPEND(DH, G) hipLaunchKernelGGL((append_kernel<DH, TI, G>), grid, dim3(256 * G), 0, stream, a, per, adv)
+    if (four) {
+        if (a.d == 32) APPEND(32, 4);
+        else if constexpr (sizeof(TI) == 2) APPEND(64, 4);
+    } else switch (a.d) {
+        case 32: APPEND(32, 1); break;
+        case 64: APPEND(64, 1); break;
+        case 128: APPEND(128, 1); break;
+        default: APPEND(256, 1); break;
     }
+#undef APPEND
     LAUNCH_CHECK();
     if (!adv) {
         hipLaunchKernelGGL(advance_kernel, dim3((a.B * a.Hkv + 255) / 256), dim3(256), 0, stream, a);

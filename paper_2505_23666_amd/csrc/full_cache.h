@@ -125,22 +125,24 @@ __device__ __forceinline__ int held(const Args &a, int si) {
 }
 
 // ---- append -------------------------------------------------------------------------------------------------
-// A workgroup takes `per` consecutive blocks of the window of blocks that a stream's new tokens fall into, one at a time: the
-// block's new rows (8 elements of a row per thread) are held in registers, the largest magnitudes are joined over the workgroup,
+// A workgroup takes `per` consecutive blocks of the window of blocks that a stream's new tokens fall into, G at a time, 256 threads each: a
+// block's new rows (8 elements of a row per thread) are held in registers, the largest magnitudes are joined over its threads,
 // rows that the block held before are rescaled only if its exponent grows.  Bound by HBM: 2 T d elements read, 2 T d codes written (4 x 32 Ki
 // tokens, 8 kv heads, d = 128: 161 us, 5.0 TB/s); a call of a few tokens is a chain of four dependent accesses, 6 us.
-template <int DH, typename TI>
-__global__ __launch_bounds__(256) void append_kernel(Args a, int per, int advance) {
+template <int DH, typename TI, int G>
+__global__ __launch_bounds__(256 * G) void append_kernel(Args a, int per, int advance) {
     constexpr int TPR = DH / 8, RPP = 256 / TPR, NP = BLK / RPP < 1 ? 1 : BLK / RPP;   // threads per row, rows per pass, passes
-    __shared__ float red[2][4];
-    const int si = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    __shared__ float red_l[G][2][4];
+    const int si = blockIdx.x, b = si / a.Hkv, h = si - b * a.Hkv, grp = threadIdx.x / 256, tid = threadIdx.x % 256, lane = tid & 63, w = tid >> 6;
+    float (*red)[4] = red_l[grp];
     const int c0 = held(a, si), told = new_tokens(a, b), n = min(told, a.cap - c0);
     const int64_t first = a.mem.n_tokens[si];
     const TI *kp = (const TI *)a.k + b * a.k_sb + h * a.k_sh, *vp = (const TI *)a.v + b * a.k_sb + h * a.k_sh;
     const int col = (tid % TPR) * 8, row0 = tid / TPR;
-    for (int i = 0; i < per; i++) {
-        const int J = c0 / BLK + blockIdx.y * per + i, lo = max(c0, J * BLK), hi = min(c0 + n, J * BLK + BLK);
-        if (lo >= hi) break;   // (uniform)
+    for (int i = 0; i < per; i += G) {
+        const int Ji = c0 / BLK + blockIdx.y * per + i, J = Ji + grp, lo = max(c0, J * BLK), hi = min(c0 + n, J * BLK + BLK);
+        if (Ji * BLK >= c0 + n) break;   // (the workgroup's; a group beyond the end goes along without rows)
+        const bool work = G == 1 || lo < hi;
         uint8_t *kc = a.mem.k + ((size_t)si * a.cap + (size_t)J * BLK) * DH, *vc = a.mem.v + ((size_t)si * a.cap + (size_t)J * BLK) * DH;
         float x[NP][8], y[NP][8], ak = 0.f, av = 0.f;
         bool bad[NP];
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(256) void append_kernel(Args a, int per, int advanc
         ak = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
         av = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
         int ek = fit_exponent(ak), ev = fit_exponent(av);
-        const int nold = max(0, c0 - J * BLK);   // rows held before
+        const int nold = work ? max(0, c0 - J * BLK) : 0;   // rows held before
         if (nold > 0) {
             const int ok = exponent_of(a.mem.ks[(size_t)si * a.nblk + J]), ov = exponent_of(a.mem.vs[(size_t)si * a.nblk + J]);
             ek = max(ek, ok); ev = max(ev, ov);
@@ -185,9 +187,9 @@ __global__ __launch_bounds__(256) void append_kernel(Args a, int per, int advanc
                 if (ek > ok) { uint2 u = reinterpret_cast<uint2 *>(kc)[e]; u.x = rescale_codes(u.x, fk); u.y = rescale_codes(u.y, fk); reinterpret_cast<uint2 *>(kc)[e] = u; }
                 if (ev > ov) { uint2 u = reinterpret_cast<uint2 *>(vc)[e]; u.x = rescale_codes(u.x, fv); u.y = rescale_codes(u.y, fv); reinterpret_cast<uint2 *>(vc)[e] = u; }
             }
-            __syncthreads();   // every thread has read the old scales
         }
-        if (tid == 0) { a.mem.ks[(size_t)si * a.nblk + J] = pow2(ek); a.mem.vs[(size_t)si * a.nblk + J] = pow2(ev); }
+        if (G > 1 || nold > 0) __syncthreads();   // every thread has read the old scales
+        if (work && tid == 0) { a.mem.ks[(size_t)si * a.nblk + J] = pow2(ek); a.mem.vs[(size_t)si * a.nblk + J] = pow2(ev); }
         const float ik = pow2(-ek), iv = pow2(-ev);
 #pragma unroll
         for (int p = 0; p < NP; p++) {
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(256) void append_kernel(Args a, int per, int advanc
     }
     if (advance) {   // this workgroup has all of the stream's blocks
         __syncthreads();   // every thread has read count and n_tokens
-        if (tid == 0) { a.mem.count[si] = c0 + n; a.mem.n_tokens[si] = first + told; }
+        if (threadIdx.x == 0) { a.mem.count[si] = c0 + n; a.mem.n_tokens[si] = first + told; }
     }
 }
 
