@@ -350,7 +350,7 @@ lola_status lola_full_evict(const lola_full_config *c, const lola_full_state *st
     const int lds = a.cap <= RANKS_LDS ? a.cap * 4 : 0;
 #define BY_DIM(K) (a.d == 32 ? K<32> : a.d == 64 ? K<64> : a.d == 128 ? K<128> : K<256>)
     // Short caches from which at most 512 pairs can move: the whole eviction of a stream in one workgroup (with the append of a
-    // turn, 16 sequences of the 8B shape with a budget of 2048 pairs 22.7 us, 24.5 by the kernels below; 128 of the 1B shape with 1111 23.8 and 28.8).
+    // turn, 16 sequences of the 8B shape with a budget of 2048 pairs 22.7 us, 24.5 by the kernels below as both were then; 128 of the 1B shape with 1111 23.8 and 28.8).
     if (a.cap <= 8192 && a.most <= 512) {
         hipLaunchKernelGGL(BY_DIM(evict_few_kernel), dim3(S), dim3(256), lds + (2 * a.most + 3 * a.nkb) * 4, (hipStream_t)stream, a);
         LAUNCH_CHECK();

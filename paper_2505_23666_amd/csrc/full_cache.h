@@ -128,7 +128,7 @@ __device__ __forceinline__ int held(const Args &a, int si) {
 // A workgroup takes `per` consecutive blocks of the window of blocks that a stream's new tokens fall into, G at a time, 256 threads each: a
 // block's new rows (8 elements of a row per thread) are held in registers, the largest magnitudes are joined over its threads,
 // rows that the block held before are rescaled only if its exponent grows.  Bound by HBM: 2 T d elements read, 2 T d codes written (4 x 32 Ki
-// tokens, 8 kv heads, d = 128: 161 us, 5.0 TB/s); a call of a few tokens is a chain of four dependent accesses, 6 us.
+// tokens, 8 kv heads, d = 128: 158 us, 5.1 TB/s); a call of a few tokens is a chain of four dependent accesses, 6 us.
 template <int DH, typename TI, int G>
 __global__ __launch_bounds__(256 * G) void append_kernel(Args a, int per, int advance) {
     constexpr int TPR = DH / 8, RPP = 256 / TPR, NP = BLK / RPP < 1 ? 1 : BLK / RPP;   // threads per row, rows per pass, passes
@@ -379,7 +379,7 @@ __device__ __forceinline__ int select_pairs(const EvictArgs &a, int si, int coun
 }
 
 // One workgroup per stream: the lists of evict_move_kernel.  Bound by latency: a handful of dependent passes over a few thousand ranks
-// (32 Ki slots of 32 streams 31 us).
+// (32 Ki slots of 32 streams 26 us).
 template <int NT>
 __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint32_t rank_l[];     // [min(cap, RANKS_LDS)] where they fit
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
 // The whole eviction of a stream by one workgroup, where few pairs can move: the lists stay in LDS, the pairs are moved side by side rather
 // than block by block.  Each pair raises its block's exponents to what it needs (an LDS maximum), blocks whose exponent grew are
 // rescaled, then the pairs are written; the scales themselves last, since a pair may come from the block that the budget ends in.
-// Bound by latency: 64 of 2112 pairs, 128 streams, d = 128 15 us; 16 of 1127, 1024 streams, d = 64 17 us.
+// Bound by latency: 64 of 2112 pairs, 128 streams, d = 128 14 us; 16 of 1127, 1024 streams, d = 64 17 us.
 template <int DH>
 __global__ __launch_bounds__(256) void evict_few_kernel(EvictArgs a) {
     constexpr int TPR = DH / 8, RPP = 256 / TPR, U = 4;      // threads per row, rows per pass, passes held in registers

@@ -10,9 +10,9 @@
 // index of each block (of long caches taken beforehand by a kernel of its own): slots need not be in the order of tokens (evictions fill holes).
 //
 // Bound by the sum of its matrix and vector instructions, of two wavefronts per SIMD, and by power: four prompts of 4096 tokens (32 query, 8 kv
-// heads, d = 128, bf16) 0.59 ms alone, 930 TFLOP/s, where a large library product reaches 1330; the same with all elements equal is a fifth
+// heads, d = 128, bf16) 0.61 ms alone, 900 TFLOP/s, where a large library product reaches 1330; the same with all elements equal is a fifth
 // faster.  A block of a wavefront is 32 products of 32 cycles, 32 exponentials, about 200 other vector instructions and 32 KB from LDS.  At
-// d = 64 the exponentials weigh as much as the products (two prompts of 2000 tokens, fp32 outputs: 72 us).
+// d = 64 the exponentials weigh as much as the products (two prompts of 2000 tokens, fp32 outputs: 70 us).
 //
 // The maximum is only moved when a logit exceeds it by more than 2^RAISE: weights then reach 2^RAISE, held times 2^SHIFT in fp16.
 #pragma once

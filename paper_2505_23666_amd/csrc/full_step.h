@@ -2,8 +2,8 @@
 // query head of the group).
 //
 // Bound by HBM: every code is read once for all rows of the group (256 bytes a slot at d = 128 against 2 x 4 x 128 x 2 flops for four heads).
-// 64 sequences of 2048 to 4096 pairs (32 query, 8 kv heads, d = 128): 81 us a step, 5.0 TB/s, where a copy reaches 4.9; one sequence of
-// 128 Ki pairs 57 us with the join.  Short caches are bound by a chain of dependent loads: 8 streams of 1500 pairs at d = 64 6.5 + 3 us.
+// 64 sequences of 2048 to 4096 pairs (32 query, 8 kv heads, d = 128): 82 us a step, 4.9 TB/s, the rate of a large copy; one sequence of
+// 128 Ki pairs 55 us with the join.  Short caches are bound by a chain of dependent loads: 8 streams of 1500 pairs at d = 64 6 + 3 us.
 // A stream's blocks are dealt to `nsplit` workgroups and within one to its wavefronts (four, or eight where one workgroup has all of a short cache); each wavefront keeps a running maximum, sum
 // and output of its own over the blocks it reads, nothing is exchanged before its last block.
 //
