@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
     constexpr int TPR = DH / 8, RPP = 256 / TPR, U = 4;      // threads per row, rows per pass, passes held
     __shared__ float red[2][4];
     const int si = blockIdx.y, w = threadIdx.x >> 6, lane = threadIdx.x & 63, tid = threadIdx.x, J = blockIdx.x;
-    const int j0 = a.before[(size_t)si * (a.nkb + 1) + J], j1 = a.before[(size_t)si * (a.nkb + 1) + J + 1];
+    const int j0 = a.before[(size_t)si * (a.nkb + 1) + J], j1 = min(a.before[(size_t)si * (a.nkb + 1) + J + 1], a.most);
     if (j0 >= j1) return;
     const int32_t *dst = a.dst + (size_t)si * a.most, *src = a.src + (size_t)si * a.most;
     const size_t base = (size_t)si * a.cap;
@@ -528,6 +528,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
         for (int u = 0; u < U; u++) {
             const int j = jb + u * RPP + tid / TPR;
             from[u] = j < j1 ? src[j] : -1;
+            if (from[u] < a.keep || from[u] >= a.cap) from[u] = -1;      // (never, unless weights change while they are ranked)
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
@@ -581,6 +582,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
             const int s = from[u];
             if (s < 0) continue;
             const int t = dst[jb + u * RPP + tid / TPR];
+            if (t < 0 || t >= a.keep) continue;
             // (a source's exponent may be larger than the block's: its codes then grow, and fit by the choice of ek, ev)
             const float fk = pow2(min(40, max(exponent_of(sk[u]) - ek, -40))), fv = pow2(min(40, max(exponent_of(sv[u]) - ev, -40)));
             uint2 c = kc[u];
