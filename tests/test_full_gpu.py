@@ -509,6 +509,54 @@ def test_graph_replays():
             assert torch.equal(getattr(a.c, n)[:, :, :256].view(torch.uint8), getattr(b.c, n)[:, :, :256].view(torch.uint8)), (t, n)
 
 
+def test_graphs_that_share_a_workspace_and_calls_side_by_side():
+    """Nothing lives in a workspace between calls: two captured graphs of different caches share one and are replayed in turn; and two
+    caches with workspaces of their own go through the same calls on two streams at once."""
+    rng = np.random.default_rng(43)
+    ps = [Pair(2, 8, 2, 64, 2048) for _ in range(4)]
+    q, k, v = (x.to(DEV) for x in ps[0].tokens(rng, 1500))
+    tok = [[x[:, :, 0].contiguous().to(DEV) for x in ps[0].tokens(rng, 1)] for _ in range(8)]
+    for p in ps:
+        p.c.append(k, v)
+        p.c.attend(q, gather=True)
+    want = []
+    for x in tok:
+        want.append(ps[0].c.step(*x, gather=True))
+        ps[0].c.evict(1400, 2, 50)
+    graphs, fixed = [], [x.clone() for x in tok[0]]
+    ps[1].c._ws(1, 1)
+    ps[2].c.workspace = ps[1].c.workspace
+    outs = [torch.empty((2, 8, 64), device=DEV) for _ in range(2)]
+    for p, out in zip(ps[1:3], outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            p.c.step(*fixed, out=out, gather=True)
+            p.c.evict(1400, 2, 50)
+    for x, y in zip(tok, want):
+        for f, z in zip(fixed, x):
+            f.copy_(z)
+        for g, out in zip(graphs, outs):
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, y)
+    # side by side with another cache on another stream
+    other = Pair(2, 8, 2, 64, 2048)
+    other.c.append(k, v)
+    other.c.attend(q, gather=True)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = ([], [])
+    torch.cuda.synchronize()
+    for x in tok:
+        for st, p, o in zip(streams, (ps[3], other), got):
+            with torch.cuda.stream(st):
+                o.append(p.c.step(*x, gather=True))
+                p.c.evict(1400, 2, 50)
+    torch.cuda.synchronize()
+    for o in got:
+        for y, z in zip(o, want):
+            assert torch.equal(y, z)
+
+
 def test_offsets_beyond_32_bits():
     """A second stream whose rows begin beyond 2^32 bytes: zero keys weigh all pairs alike, so the output is the mean of the values."""
     cap, d = 1 << 24, 256
