@@ -146,6 +146,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         if (t < n) load_query((const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st + s * 16 + hi * 8, qf[s]);
         else zero_query<QP>(qf[s]);
     }
+    if constexpr (QP == 1) spoil_query<NK>(qf[0]);
     f16v o[ND];
 #pragma unroll
     for (int d = 0; d < ND; d++)

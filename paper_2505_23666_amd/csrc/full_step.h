@@ -48,16 +48,17 @@ __device__ __forceinline__ h8 codes_to_f16(uint32_t a, uint32_t b, float scale) 
 __device__ __forceinline__ i2 lds_read_tr8(const uint8_t *p) {
     return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i2 *)(p));
 }
-// x as three bf16 parts whose sum it is: 8 of its 24 bits each, cut off rather than rounded, so that no part overflows
+// x as three bf16 parts whose sum it is: 8 of its 24 bits each, cut off rather than rounded, so that no part overflows.  What is not finite
+// becomes NaN (see spoil_query).
 __device__ __forceinline__ void split_bf16(const float *x, bf8 *part) {
 #pragma unroll
     for (int e = 0; e < 8; e++) {
         float r = x[e];
 #pragma unroll
         for (int p = 0; p < 3; p++) {
-            const uint32_t u = __float_as_uint(r) & 0xFFFF0000u;
+            const uint32_t u = finite(r) ? __float_as_uint(r) & 0xFFFF0000u : 0x7FC00000u;
             part[p][e] = __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
-            r = finite(r) ? r - __uint_as_float(u) : 0.f;      // (NaN and infinities stay in the first part; a NaN may become infinite there: its row is NaN all the same)
+            r = finite(r) ? r - __uint_as_float(u) : 0.f;
         }
     }
 }
@@ -105,6 +106,20 @@ __device__ __forceinline__ void load_query(const float *p, bf8 *part) {
     float x[8];
     load8(p, x);
     split_bf16(x, part);
+}
+// A query with an element that is not finite has the output NaN wherever it sees a pair: an infinite element makes each of its logits infinite
+// or NaN, and a softmax of infinities is NaN, also where all of them are negative and would pass for weights of zero.  So one such element
+// among a lane's N operands makes the first operand NaN, and with it every logit of the row.  (Two elements at a time: an exponent of
+// ones carries into the sign's place.)
+template <int N>
+__device__ __forceinline__ void spoil_query(bf8 *q) {
+    uint32_t carry = 0;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const uint4 u = __builtin_bit_cast(uint4, q[i]);
+        carry |= ((u.x & 0x7F807F80u) + 0x00800080u) | ((u.y & 0x7F807F80u) + 0x00800080u) | ((u.z & 0x7F807F80u) + 0x00800080u) | ((u.w & 0x7F807F80u) + 0x00800080u);
+    }
+    if (carry & 0x80008000u) q[0] = __builtin_bit_cast(bf8, make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u));
 }
 template <int QP>
 __device__ __forceinline__ void zero_query(bf8 *part) {
@@ -234,6 +249,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
             if (t < n) load_query(qp + (DH == 32 ? quad * 8 : (s / 2) * 64 + quad * 16 + (s & 1) * 8), qf[ct][s]);
             else zero_query<QP>(qf[ct][s]);
         }
+        if constexpr (QP == 1) spoil_query<NK>(qf[ct][0]);
     }
     f4 o[CT][ND];
     float m[CT], l[CT], vref = 0.f;             // o is held in units of vref, the largest scale of values so far
