@@ -35,8 +35,6 @@ struct Args {
 
 __device__ __forceinline__ int exponent_of(float scale) { return (int)((__float_as_uint(scale) >> 23) & 255u) - 127; }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
-// 1 / x for a power of two (2^-126 .. 2^126)
-__device__ __forceinline__ float inv_pow2(float x) { return __uint_as_float(0x7F000000u - (__float_as_uint(x) & 0x7F800000u)); }
 
 // least e >= EXP_MIN with a <= 448 * 2^e, a >= 0 finite: 448 = 1.75 * 2^8, a = 1.f * 2^x (a below 2^-126 is below every bound)
 __device__ __forceinline__ int fit_exponent(float a) {

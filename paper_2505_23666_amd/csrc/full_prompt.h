@@ -3,8 +3,8 @@
 //
 // One workgroup takes 32 NW rows of a stream, wavefront w the 32 from 32 w on, and goes over the blocks of 64 slots that any of them may
 // see; where there are few rows, the blocks are dealt to several workgroups and their shares joined.  A block's codes are loaded
-// into registers while the one before it is worked on, converted once for all rows and put into the other of two LDS buffers: keys as bf16, values as fp16
-// relative to the largest scale so far (both exact, up to fp16's range).  Products are 32x32x16 and transposed: S^T = K Q^T has a query per
+// into registers while the one before it is worked on, converted once for all rows and put into the other of two LDS buffers: keys as bf16 with their scale, values'
+// codes as fp16 (both exact); the values' scales enter by the weights (RowRef).  Products are 32x32x16 and transposed: S^T = K Q^T has a query per
 // lane pair, so the running maximum and sum live there, and its C layout is the B layout of O^T += V^T P^T, whose V^T comes from the
 // transposing 16-bit LDS read.  Which blocks can be passed over and which need a comparison per element follows from the least and largest token
 // index of each block (of long caches taken beforehand by a kernel of its own): slots need not be in the order of tokens (evictions fill holes).
@@ -14,7 +14,8 @@
 // faster.  A block of a wavefront is 32 products of 32 cycles, 32 exponentials, about 200 other vector instructions and 32 KB from LDS.  At
 // d = 64 the exponentials weigh as much as the products (two prompts of 2000 tokens, fp32 outputs: 70 us).
 //
-// The maximum is only moved when a logit exceeds it by more than 2^RAISE: weights then reach 2^RAISE, held times 2^SHIFT in fp16.
+// The row's references (RowRef) are only moved when a logit exceeds them by more than RAISE: weights (times scales) then reach 2^RAISE, held times
+// 2^SHIFT in fp16.
 #pragma once
 #include <type_traits>
 #include "full_step.h"
@@ -32,7 +33,7 @@ struct PromptArgs {
     int nsplit, ntiles;
     int2 *span;        // [S][nblk] least and largest token index of each block; NULL: up to 64 blocks, each workgroup looks at the indices
     float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
-    float *part_ml;    // [S][nsplit][R][2] maximum (powers of two) and sum
+    float *part_ml;    // [S][nsplit][R][2] RowRef::m and sum
     float *stat;       // [S][R] maximum + log2 of the sum (infinite: the row adds no weight), where weights are gathered
 };
 
@@ -152,7 +153,8 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     for (int d = 0; d < ND; d++)
 #pragma unroll
         for (int e = 0; e < 16; e++) o[d][e] = 0.f;
-    float m = -INFINITY, l = 0.f;          // (l: this lane's half of the row)
+    RowRef ref;
+    float l = 0.f;          // (this lane's half of the row)
 
     uint4 kr[NL], vr[NL];
     int idr = 0;
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
                 vr[i] = *reinterpret_cast<const uint4 *>(vp + (i * NTHR + tid) * 16);
             }
     };
-    auto store = [&](uint8_t *buf, int J, float kscale, float vscale) {
+    auto store = [&](uint8_t *buf, int J, float kscale) {
         const int live = count - J * BLK;
         if (tid < BLK) reinterpret_cast<int *>(buf + 2 * HALF)[tid] = tid < live ? idr : 0x7FFFFFFF;    // (no pair: later than all queries)
 #pragma unroll
@@ -177,8 +179,8 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
                 *reinterpret_cast<bf8 *>(kp + ((pc ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].x, kr[i].y, kscale);
                 *reinterpret_cast<bf8 *>(kp + (((pc + 1) ^ kswz2<DH>(row)) * 16)) = codes_to_bf16(kr[i].z, kr[i].w, kscale);
                 if (row >= live) vr[i] = make_uint4(0, 0, 0, 0);      // slots without a pair hold zeros
-                *reinterpret_cast<h8 *>(vp + ((pc ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].x, vr[i].y, vscale);
-                *reinterpret_cast<h8 *>(vp + (((pc + 1) ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].z, vr[i].w, vscale);
+                *reinterpret_cast<h8 *>(vp + ((pc ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].x, vr[i].y);
+                *reinterpret_cast<h8 *>(vp + (((pc + 1) ^ vswz2<DH>(row)) * 16)) = codes_to_f16(vr[i].z, vr[i].w);
             }
     };
 
@@ -189,13 +191,13 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     }
     const float c = a.scale2;
     const float minus_one = opaque_minus_one();
-    float vref = 0.f, vstage = 0.f;      // o is in units of vref; the staged block's values in units of vstage
+    float ev = 0.f;      // exponent of the staged block's values
     bool masked = false;
     if (J < J1) {
         load(J);
-        vstage = lane_of_f(vsT, J);
+        ev = (float)exponent_of(lane_of_f(vsT, J));
         masked = (int64_t)lane_of(spT.y, J) > w_first;
-        store(lds, J, lane_of_f(ksT, J), 1.f);
+        store(lds, J, lane_of_f(ksT, J));
     }
     lds_barrier();
     auto block = [&](auto which) {
@@ -236,34 +238,36 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
 #pragma unroll
             for (int e = 0; e < 16; e++) mb = fmaxf(mb, s[kt][e]);
         mb *= c;
-        if (__any(mb > m + RAISE || (m == -INFINITY && mb > m))) {
-            mb = half_max(mb);
-            const float mn = fmaxf(m, mb), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-            m = mn; l *= f;
+        if (__any(mb - ref.m > RAISE + fminf(ref.x - ev, 0.f))) {
+            float fl, fo;
+            ref.move(half_max(mb), ev, fl, fo);
+            l *= fl;
 #pragma unroll
-            for (int d = 0; d < ND; d++) o[d] *= f;
+            for (int d = 0; d < ND; d++) o[d] *= fo;
         }
-        if (vstage > vref) {      // (uniform; rare beyond the first block)
-            const float f = vref * inv_pow2(vstage);
+        const float drop = ref.drop(ev);
+        float cs = c, off = ref.m + (drop - SHIFT);
+        if (__any(ref.far())) {
+            cs = 1.f; off = drop - SHIFT;
 #pragma unroll
-            for (int d = 0; d < ND; d++) o[d] *= f;
-            vref = vstage;
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) s[kt][e] = fmaf(s[kt][e], c, -ref.m);
         }
-        const float off = (m == -INFINITY ? 0.f : m) - SHIFT;
         h8 pf[4][PP];
         float sum = 0.f;
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), y = __builtin_amdgcn_exp2f(fmaf(s[kt][e + 1], c, -off));
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[kt][e], cs, -off)), y = __builtin_amdgcn_exp2f(fmaf(s[kt][e + 1], cs, -off));
                 sum += x; sum += y;
                 h2 part[PP];
                 to_f16_parts<PP>(x, y, minus_one, part);
 #pragma unroll
                 for (int p = 0; p < PP; p++) { pf[kt * 2 + e / 8][p][e & 7] = part[p][0]; pf[kt * 2 + e / 8][p][(e & 7) + 1] = part[p][1]; }
             }
-        l += sum;
+        l = fmaf(sum, __builtin_amdgcn_exp2f(drop), l);
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             const int j = lane & 15, key = k * 16 + hi * 4 + (j >> 2);
@@ -282,10 +286,9 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
             }
         }
         if (Jn < J1) {
-            const float v = lane_of_f(vsT, Jn);
-            vstage = fmaxf(vstage, v);
+            ev = (float)exponent_of(lane_of_f(vsT, Jn));
             masked = (int64_t)lane_of(spT.y, Jn) > w_first;
-            store(lds + (CUR ^ 1) * BUF, Jn, lane_of_f(ksT, Jn), v * inv_pow2(vstage));
+            store(lds + (CUR ^ 1) * BUF, Jn, lane_of_f(ksT, Jn));
         }
         lds_barrier();
         J = Jn;
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     l = half_sum(l);
     if (r < R) {
         const bool pad = t >= n;
-        const float il = pad || l == 0.f ? 0.f : vref / l;
+        const float il = pad || l == 0.f ? 0.f : 1.f / l, unit = __builtin_amdgcn_exp2f(ref.x);
         auto put = [&](auto *op) {
 #pragma unroll
             for (int d = 0; d < ND; d++)
@@ -306,17 +309,17 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
                 for (int q = 0; q < 4; q++) {
                     f4 u;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) u[e] = il == 0.f ? 0.f : o[d][q * 4 + e] * il;
+                    for (int e = 0; e < 4; e++) u[e] = il == 0.f ? 0.f : o[d][q * 4 + e] * il * unit;
                     store4(op + d * 32 + q * 8 + hi * 4, u);
                 }
         };
         if (pa.nsplit == 1) {
             put((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st);
-            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = (!pad && l > 0.f && finite(l)) ? m + __builtin_amdgcn_logf(l) - SHIFT : INFINITY;
+            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = (!pad && l > 0.f && finite(l)) ? ref.m + __builtin_amdgcn_logf(l) - SHIFT : INFINITY;
         } else {
             const size_t at = ((size_t)si * pa.nsplit + split) * R + r;
             put(pa.part_o + at * DH);
-            if (hi == 0) { pa.part_ml[at * 2] = m; pa.part_ml[at * 2 + 1] = pad ? 0.f : l; }
+            if (hi == 0) { pa.part_ml[at * 2] = ref.m; pa.part_ml[at * 2 + 1] = pad ? 0.f : l; }
         }
     }
 }

@@ -11,10 +11,10 @@
 //   S^T = K Q^T   16x16x32 bf16: keys (codes times scale) are exact in bf16, so are bf16 queries; fp32 queries enter as three bf16 parts (24 bits).  A lane's
 //                 operand is eight consecutive bytes of its key row, straight from global memory: the order of the contraction
 //                 index is free as long as the queries are laid out the same.
-//   p = 2^(s - m + 14), rounded to fp16 (fp32 outputs: two fp16 parts): the operand of the second product.  The shift keeps weights down
-//                 to 2^-28 of the largest among fp16's normal numbers; the sum takes p before the rounding.
-//   O^T += V^T P^T  16x16x32 fp16: V's codes are exact in fp16 and are converted with their block's scale relative to the
-//                 largest so far; the codes pass through LDS for the transposing 8-bit read, 16-byte pieces XOR-swizzled
+//   p = 2^(s - m + 14) times the values' scale in units of 2^x, rounded to fp16 (fp32 outputs: two fp16 parts): the operand of the second product.
+//                 m (the maximum rounded up) and x are whole numbers of the row's own, see RowRef.  The shift keeps products of weight and scale
+//                 down to 2^-28 of the row's largest among fp16's normal numbers; the sum takes p before the rounding.
+//   O^T += V^T P^T  16x16x32 fp16: V's codes, exact in fp16; they pass through LDS for the transposing 8-bit read, 16-byte pieces XOR-swizzled
 //                 by row so that the 32 rows of a read meet all banks alike.  The C layout of the first product is the B layout of this one.
 #pragma once
 #include "full_cache.h"
@@ -38,11 +38,11 @@ __device__ __forceinline__ bf8 codes_to_bf16(uint32_t a, uint32_t b, float scale
     u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
     return u.v;
 }
-// eight codes times a power of two <= 1 -> eight fp16 (exact down to fp16's least number)
-__device__ __forceinline__ h8 codes_to_f16(uint32_t a, uint32_t b, float scale) {
+// eight codes -> eight fp16 (exact)
+__device__ __forceinline__ h8 codes_to_f16(uint32_t a, uint32_t b) {
     union { h8 v; h2 p[4]; } u;
-    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, false); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, true);
-    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, false); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, true);
+    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
     return u.v;
 }
 __device__ __forceinline__ i2 lds_read_tr8(const uint8_t *p) {
@@ -81,11 +81,30 @@ __device__ __forceinline__ float opaque_minus_one() {
     return x;
 }
 
+// A row's references, whole numbers.  m: its sum of weights is held times 2^-m.  x: its output is held times 2^(-m - x), x being such that of the
+// row's products of a weight and a block's scale (2^(s - m) 2^ev) the largest so far is about 2^x.  So the scales enter by the weights, row
+// by row, and values of a block that the row does not see, or hardly, take no bits from the others.
+struct RowRef {
+    float m = -3.4028234663852886e38f, x = -200.f;     // (nothing seen: finite, so that differences are)
+    __device__ __forceinline__ bool seen() const { return m != -3.4028234663852886e38f; }
+    // Moves on to a block whose largest logit is mb (-inf: none) and whose values have the exponent ev; by what the sum and the output then shrink.
+    __device__ __forceinline__ void move(float mb, float ev, float &fl, float &fo) {
+        const float top = ceilf(mb), mn = fmaxf(m, top), xn = fmaxf(x + (m - mn), (top - mn) + ev);
+        fl = __builtin_amdgcn_exp2f(m - mn);
+        fo = __builtin_amdgcn_exp2f((m - mn) + (x - xn));
+        m = mn; x = xn;
+    }
+    // The block's weights are to be held times 2^(shift - m - drop()).  From 2^64 below the row's largest products on they are nothing in fp16 anyway.
+    __device__ __forceinline__ float drop(float ev) const { return fminf(x - ev, 64.f); }
+    // m + drop - shift is no whole number any more: the logits are to be taken relative to m first
+    __device__ __forceinline__ bool far() const { return fabsf(m) >= 4194304.f && seen(); }
+};
+
 struct StepArgs {
     Args a;
     int nsplit;
     float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
-    float *part_ml;    // [S][nsplit][R][2] running maximum (powers of two) and sum; sum 0: an empty share
+    float *part_ml;    // [S][nsplit][R][2] RowRef::m and sum; sum 0: an empty share
     float *logit;      // [S][R][cap] logits (powers of two) where weights are gathered, else NULL
     int32_t *counts;   // [S] with a token appended by the same launch and weights gathered: the slots in use after it
     int append;        // the join moves the counters on (a.k, a.v hold the token)
@@ -188,7 +207,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
     constexpr int VI = DH / 16;                     // 16-byte loads per lane of a block's values
     constexpr int PR = DH / 16;                     // pieces per row
     __shared__ __attribute__((aligned(16))) uint8_t stage[NW][BLK * DH];
-    __shared__ float ml_l[NW][2][16 * CT], vref_l[NW];
+    __shared__ float ml_l[NW][3][16 * CT];
     const Args &a = sa.a;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
     const int si = blockIdx.x, split = blockIdx.y, b = si / a.Hkv, h = si - b * a.Hkv;
@@ -252,10 +271,11 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
         if constexpr (QP == 1) spoil_query<NK>(qf[ct][0]);
     }
     f4 o[CT][ND];
-    float m[CT], l[CT], vref = 0.f;             // o is held in units of vref, the largest scale of values so far
+    RowRef ref[CT];
+    float l[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ct++) {
-        m[ct] = -INFINITY; l[ct] = 0.f;
+        l[ct] = 0.f;
 #pragma unroll
         for (int c = 0; c < ND; c++) o[ct][c] = (f4){0.f, 0.f, 0.f, 0.f};
     }
@@ -265,8 +285,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
         if (it == 64) { it = 0; scales(J); }
         const float ksJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksT), it)), vsJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsT), it));
         const int live = count - J * BLK;          // slots of this block that hold pairs (64 and more: all)
-        const float c = a.scale2, vnew = fmaxf(vref, vsJ), iv = inv_pow2(vnew), vscale = vsJ * iv, vkeep = vref * iv;
-        vref = vnew;
+        const float c = a.scale2, ev = (float)exponent_of(vsJ);
         // values to LDS; slots without a pair hold zeros there
 #pragma unroll
         for (int i = 0; i < VI; i++) {
@@ -311,24 +330,32 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
 #pragma unroll
                 for (int t = 0; t < 4; t++) *reinterpret_cast<f4 *>(lp + t * 16) = s[ct][t];
             }
-            mb = quad_max(mb);
-            const float mn = fmaxf(m[ct], mb), mu = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m[ct] - mu);   // (m = -inf: 0)
-            m[ct] = mn;
+            float fl, fo;
+            ref[ct].move(quad_max(mb), ev, fl, fo);
+            const float t = ref[ct].drop(ev);
+            float off = ref[ct].m + (t - P_SHIFT);
+            if (__any(ref[ct].far())) {
+                off = t - P_SHIFT;
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) s[ct][k][e] -= ref[ct].m;
+            }
             float sum = 0.f;
 #pragma unroll
-            for (int t = 0; t < 4; t++)
+            for (int k = 0; k < 4; k++)
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
-                    const float x = __builtin_amdgcn_exp2f(s[ct][t][e] - (mu - P_SHIFT)), y = __builtin_amdgcn_exp2f(s[ct][t][e + 1] - (mu - P_SHIFT));
+                    const float x = __builtin_amdgcn_exp2f(s[ct][k][e] - off), y = __builtin_amdgcn_exp2f(s[ct][k][e + 1] - off);
                     sum += x + y;
                     h2 part[PP];
                     to_f16_parts<PP>(x, y, minus_one, part);
 #pragma unroll
-                    for (int p = 0; p < PP; p++) { pf[ct][t / 2][p][(t & 1) * 4 + e] = part[p][0]; pf[ct][t / 2][p][(t & 1) * 4 + e + 1] = part[p][1]; }
+                    for (int p = 0; p < PP; p++) { pf[ct][k / 2][p][(k & 1) * 4 + e] = part[p][0]; pf[ct][k / 2][p][(k & 1) * 4 + e + 1] = part[p][1]; }
                 }
-            l[ct] = l[ct] * f + quad_sum(sum);
+            l[ct] = l[ct] * fl + quad_sum(sum) * __builtin_amdgcn_exp2f(t);
 #pragma unroll
-            for (int d = 0; d < ND; d++) o[ct][d] *= f * vkeep;
+            for (int d = 0; d < ND; d++) o[ct][d] *= fo;
         }
 #pragma unroll
         for (int k = 0; k < 2; k++) {
@@ -336,7 +363,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
 #pragma unroll
             for (int d = 0; d < ND; d++) {
                 const i2 u = lds_read_tr8(st + row * DH + ((d ^ vswz<DH>(row)) * 16) + (n16 & 1) * 8);
-                const h8 vf = codes_to_f16((uint32_t)u[0], (uint32_t)u[1], vscale);
+                const h8 vf = codes_to_f16((uint32_t)u[0], (uint32_t)u[1]);
 #pragma unroll
                 for (int ct = 0; ct < CT; ct++)
 #pragma unroll
@@ -345,11 +372,10 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
         }
     }
 
-    // the wavefronts' shares: O^T [column][row] in turn through the staging memory, weighted by their maxima
-    if (lane == 0) vref_l[w] = vref;
+    // the wavefronts' shares: O^T [column][row] in turn through the staging memory, weighted by their references
     if (quad == 0)
 #pragma unroll
-        for (int ct = 0; ct < CT; ct++) { ml_l[w][0][ct * 16 + n16] = m[ct]; ml_l[w][1][ct * 16 + n16] = l[ct]; }
+        for (int ct = 0; ct < CT; ct++) { ml_l[w][0][ct * 16 + n16] = ref[ct].m; ml_l[w][1][ct * 16 + n16] = l[ct]; ml_l[w][2][ct * 16 + n16] = ref[ct].x; }
     __syncthreads();
     if (APPEND && tid == 0) {
         if (!sa.part_ml) { a.mem.count[si] = count; a.mem.n_tokens[si] += 1; }       // (the stream's only workgroup)
@@ -370,19 +396,15 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
             float M = -INFINITY;
 #pragma unroll
             for (int i = 0; i < NW; i++) M = fmaxf(M, ml_l[i][0][r]);
-            const float mu = M == -INFINITY ? 0.f : M;
-            float L = 0.f, f[NW], y = 0.f;
+            float L = 0.f, y = 0.f;
 #pragma unroll
-            for (int i = 0; i < NW; i++) {
-                f[i] = __builtin_amdgcn_exp2f(ml_l[i][0][r] - mu);
-                L += ml_l[i][1][r] * f[i];
-            }
+            for (int i = 0; i < NW; i++) L += ml_l[i][1][r] * __builtin_amdgcn_exp2f(ml_l[i][0][r] - M);
             const int t = r / a.g, hq = h * a.g + (r - t * a.g);
             if (t >= n) L = 0.f;     // padding
             if (L != 0.f) {
                 const float iL = 1.f / L;
 #pragma unroll
-                for (int i = 0; i < NW; i++) y += ol[(i * DH + col) * 16 + r16] * f[i] * iL * vref_l[i];
+                for (int i = 0; i < NW; i++) y += ol[(i * DH + col) * 16 + r16] * iL * __builtin_amdgcn_exp2f((ml_l[i][0][r] - M) + ml_l[i][2][r]);
             }
             if (sa.nsplit == 1) stf((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st, col, y);
             else sa.part_o[(((size_t)si * sa.nsplit + split) * R + r) * DH + col] = y;
