@@ -101,7 +101,7 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
         p.off_span = off; if (p.span) off += up(S * (c->capacity / BLK) * 8);
         p.off_o = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * c->head_dim * 4);
         p.off_ml = off; if (p.nsplit > 1) off += up(S * p.nsplit * R * 2 * 4);
-        p.off_stat = off; if (gather) off += up(S * R * 4);
+        p.off_stat = off; if (gather) off += up(S * R * 8);
     }
     p.bytes = off;
     return p;
@@ -193,7 +193,7 @@ lola_status launch_attend(const Args &a, const AttendPlan &p, int gather, char *
     pa.span = p.span ? (int2 *)(ws + p.off_span) : nullptr;
     pa.part_o = p.nsplit > 1 ? (float *)(ws + p.off_o) : nullptr;
     pa.part_ml = p.nsplit > 1 ? (float *)(ws + p.off_ml) : nullptr;
-    pa.stat = gather ? (float *)(ws + p.off_stat) : nullptr;
+    pa.stat = gather ? (float2 *)(ws + p.off_stat) : nullptr;
     const int S = a.B * a.Hkv, R = a.T * a.g;
     constexpr int LDS = 4 * BLK * DH * 2 + 2 * BLK * 4;
     if (p.span) {

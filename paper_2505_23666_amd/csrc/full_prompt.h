@@ -34,7 +34,7 @@ struct PromptArgs {
     int2 *span;        // [S][nblk] least and largest token index of each block; NULL: up to 64 blocks, each workgroup looks at the indices
     float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
     float *part_ml;    // [S][nsplit][R][2] RowRef::m and sum
-    float *stat;       // [S][R] maximum + log2 of the sum (infinite: the row adds no weight), where weights are gathered
+    float2 *stat;      // [S][R] weight_stat(), where weights are gathered
 };
 
 // least and largest token index of each block in use; slots without a pair count as later than all queries
@@ -58,6 +58,15 @@ __device__ __forceinline__ h4 lds_read_tr16(const _Float16 *p) {
 // swizzles of the 16-byte pieces of the rows in LDS (DH 2-byte numbers): 32 rows, one piece each (keys), and 4 rows x 64 bytes (values)
 template <int DH> __device__ __forceinline__ int kswz2(int row) { return DH >= 128 ? row & 15 : DH == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 template <int DH> __device__ __forceinline__ int vswz2(int row) { return DH >= 128 ? (row & 3) << 2 : DH == 64 ? (row & 2) << 1 : 0; }
+
+// What the weights of a row are made of, p = 2^(logit - .x) .y: .x the next whole number above the sum's logarithm (no logit exceeds it), .y, from 1
+// to 2, what is left of 1 / sum.  (As one number, m + log2 of the sum, the logarithm's error would be the same for all of the row's weights and lean to one
+// side over the rows: 3.2e-7 of the weights' 2-norm, so 0.5e-7.)  m, l: reference and sum of the row, the latter held times 2^SHIFT.  A row
+// without pairs, or whose sum is not finite, adds no weight.
+__device__ __forceinline__ float2 weight_stat(float m, float l) {
+    const float n = m + ((float)exponent_of(l) + 1.f - SHIFT);
+    return l > 0.f && finite(l) ? make_float2(n, __builtin_amdgcn_exp2f((n - m) + SHIFT) / l) : make_float2(INFINITY, 0.f);
+}
 
 // four values to consecutive elements of an output row
 __device__ __forceinline__ void store4(float *p, f4 v) { *reinterpret_cast<f4 *>(p) = v; }
@@ -315,7 +324,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         };
         if (pa.nsplit == 1) {
             put((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st);
-            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = (!pad && l > 0.f && finite(l)) ? ref.m + __builtin_amdgcn_logf(l) - SHIFT : INFINITY;
+            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = weight_stat(ref.m, pad ? 0.f : l);
         } else {
             const size_t at = ((size_t)si * pa.nsplit + split) * R + r;
             put(pa.part_o + at * DH);
@@ -345,7 +354,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs pa) {
     TO *op = (TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st;
 #pragma unroll
     for (int e = 0; e < 4; e++) stf(op, col + e, L == 0.f ? 0.f : acc[e] / L);
-    if (pa.stat && col == 0) pa.stat[(size_t)si * R + r] = (L > 0.f && finite(L)) ? mu + __builtin_amdgcn_logf(L) - SHIFT : INFINITY;
+    if (pa.stat && col == 0) pa.stat[(size_t)si * R + r] = weight_stat(mu, L);
 }
 
 // sum over the 32 lanes of a half wavefront, in each of them
@@ -355,7 +364,7 @@ __device__ __forceinline__ float sum32(float v) {
     return t.a + t.b;
 }
 
-// weight[j] += sum over rows of 2^(logit - stat): one workgroup per block of slots, whose keys stay in registers as the first operand of
+// weight[j] += sum over rows of their weight of pair j (weight_stat): one workgroup per block of slots, whose keys stay in registers as the first operand of
 // S^T = K Q^T; the wavefronts take 32 rows in turn, straight from global memory, and join their sums at the end.  Bound by vector
 // instructions: an exponential and three others per logit (two prompts of 2000 tokens at d = 64: 57 us, 16.4 GFLOP).
 template <int DH, typename TI>
@@ -392,10 +401,10 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
         int r = first + w * 32 + l32, t = r / a.g, hd = r - t * a.g;
         const int t_step = 128 / a.g, h_step = 128 - t_step * a.g;
         bf8 qf[NK][QP];
-        float st = INFINITY;
+        float2 st;
         auto load = [&]() {
             const TI *qp = (const TI *)a.q + b * a.q_sb + (h * a.g + hd) * a.q_sh + t * a.q_st + hi * 8;
-            st = r < rows ? pa.stat[(size_t)si * R + r] : INFINITY;
+            st = r < rows ? pa.stat[(size_t)si * R + r] : make_float2(INFINITY, 0.f);
 #pragma unroll
             for (int k = 0; k < NK; k++) {
                 if (r < rows) load_query(qp + k * 16, qf[k]);
@@ -405,7 +414,7 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
         load();
         for (int r0 = first + w * 32; r0 < rows; r0 += 128) {
             const int pos = (int)(pos0 + t);
-            const float off = st;
+            const float off = st.x, part = st.y;
             f16v s[2];
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
@@ -421,7 +430,7 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
             r += 128; t += t_step; hd += h_step;
             if (hd >= a.g) { hd -= a.g; t++; }
             load();
-            // a weight is in [0, 1]; the clamp, an output modifier of the exponential, makes 0 of what rows without weight (off infinite) make of a NaN key
+            // the power is in [0, 1]; the clamp, an output modifier of the exponential, makes 0 of what rows without weight (off infinite) make of a NaN key
             if (masked) {
 #pragma unroll
                 for (int kt = 0; kt < 2; kt++)
@@ -438,7 +447,7 @@ __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void p
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) acc[kt][e] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), 0.f, 1.f);
+                for (int e = 0; e < 16; e++) acc[kt][e] = fmaf(__builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), 0.f, 1.f), part, acc[kt][e]);
         }
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)

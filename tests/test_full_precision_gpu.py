@@ -78,3 +78,23 @@ def test_far_logits(d, dtype, out):
         y = c.attend(q).double()
         want, _ = fd.attend(c, q)
         assert fd.distance(y, want) <= NORM[out], (B, Hq, cap, held, T, fd.distance(y, want))
+
+
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_distance_of_gathered_weights(d, dtype):
+    """A weight is off by its own exponential and normaliser (2^-23 each) and by what its logit is off (as above), which differ in sign from row to
+    row: over a few hundred rows below 1.5e-7 (2^-22.7); a normaliser that errs to one side does not average out.  Of single steps 1e-6, as outputs."""
+    for Hq, Hkv, cap, held, T in ((4, 2, 192, 150, 1), (8, 1, 4096, 3000, 1), (4, 1, 2048, 1000, 4), (8, 2, 1024, 0, 1000), (8, 2, 4096, 3000, 260)):
+        rng = np.random.default_rng(d + held + 1)
+        c = lb.LolaFullCache(2, Hq, Hkv, d, cap, dtype=dtype, device=DEV)
+        if held:
+            c.append(tokens(rng, (2, Hkv, held, d), dtype, 1.3), tokens(rng, (2, Hkv, held, d), dtype))
+        q, k, v = tokens(rng, (2, Hq, T, d), dtype), tokens(rng, (2, Hkv, T, d), dtype, 1.3), tokens(rng, (2, Hkv, T, d), dtype)
+        c.append(k, v)
+        c.attend(q, gather=True)
+        _, want = fd.attend(c, q)
+        n = held + T
+        off = fd.distance(c.weight[:, :, :n], want[:, :, :n])
+        print(f"weights d {d} {dtype} {(Hq, Hkv, cap, held, T)}: {off:.3g}", flush=True)
+        assert off <= (1e-6 if T < 10 else 1.5e-7), (Hq, Hkv, cap, held, T, off)
