@@ -301,7 +301,7 @@ lola_status lola_full_append(const lola_full_config *cfg, const lola_full_state 
  * the pairs whose idx is at most that.  All query heads of a group read the same cache:
  *   y_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j) / sum_j exp(scale q_i.k_j).
  * A query that sees nothing, and the rows i >= n, get zeros.  A query with an element that is not finite gets NaN if it sees anything.
- * (Terms below 2^-32 of the largest product of a weight that the row gives and 448 times the scale of that pair's block may be lost.)
+ * (Terms below 2^-36 of the largest product of a weight that the row gives and 448 times the scale of that pair's block may be lost.)
  * gather = 1 adds sum over the group's query heads and i < n of p_ij to weight[j]; queries whose output is NaN add nothing.
  * q, out [B, Hq, T, d] (or tokens first).  T >= 0; T * (Hq / Hkv) at most 2^24, B * Hq * T at most 2^30 (also in lola_full_append).
  */

@@ -14,8 +14,8 @@
 // faster.  A block of a wavefront is 32 products of 32 cycles, 32 exponentials, about 200 other vector instructions and 32 KB from LDS.  At
 // d = 64 the exponentials weigh as much as the products (two prompts of 2000 tokens, fp32 outputs: 70 us).
 //
-// The row's references (RowRef) are only moved when a logit exceeds them by more than RAISE: weights (times scales) then reach 2^RAISE, held times
-// 2^SHIFT in fp16.
+// The row's references (RowRef) are only moved when a logit exceeds them by more than `raise`: weights (times scales) then reach 2^raise, held times
+// 2^shift in fp16 (Slack).
 #pragma once
 #include <type_traits>
 #include "full_step.h"
@@ -26,7 +26,11 @@ namespace full {
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 
-constexpr float RAISE = 8.f, SHIFT = 7.f;
+// The 15 powers of two that fp16 has above 1, dealt to raise and shift.  The fewer to raise, the more often the references move; the more to shift, the
+// more bits small weights keep, which are all of an output where one pair takes nearly all the weight and has hardly a value (2^-17 beside such a
+// pair, fp32 outputs: off by 7e-6 to 2e-5 at raise 8, 1e-6 to 2.5e-6 at 4, 5e-7 to 8e-7 at 2; 2^-26, bf16 outputs: 1e-2 at 8, the output's own rounding at 4).
+// Four prompts of 4096 tokens (d = 128, bf16) 629, 628, 633 and 640 us at raise 8, 4, 2, 1; two of 2000 with weights (d = 64, fp32 outputs) 129, 129, 131, 132.
+template <typename TO> struct Slack { static constexpr float raise = sizeof(TO) == 4 ? 2.f : 4.f, shift = 15.f - raise; };
 
 struct PromptArgs {
     Args a;
@@ -61,11 +65,11 @@ template <int DH> __device__ __forceinline__ int vswz2(int row) { return DH >= 1
 
 // What the weights of a row are made of, p = 2^(logit - .x) .y: .x the next whole number above the sum's logarithm (no logit exceeds it), .y, from 1
 // to 2, what is left of 1 / sum.  (As one number, m + log2 of the sum, the logarithm's error would be the same for all of the row's weights and lean to one
-// side over the rows: 3.2e-7 of the weights' 2-norm, so 0.5e-7.)  m, l: reference and sum of the row, the latter held times 2^SHIFT.  A row
+// side over the rows: 3.2e-7 of the weights' 2-norm, so 0.5e-7.)  m, l: reference and sum of the row, the latter held times 2^shift.  A row
 // without pairs, or whose sum is not finite, adds no weight.
-__device__ __forceinline__ float2 weight_stat(float m, float l) {
-    const float n = m + ((float)exponent_of(l) + 1.f - SHIFT);
-    return l > 0.f && finite(l) ? make_float2(n, __builtin_amdgcn_exp2f((n - m) + SHIFT) / l) : make_float2(INFINITY, 0.f);
+__device__ __forceinline__ float2 weight_stat(float m, float l, float shift) {
+    const float n = m + ((float)exponent_of(l) + 1.f - shift);
+    return l > 0.f && finite(l) ? make_float2(n, __builtin_amdgcn_exp2f((n - m) + shift) / l) : make_float2(INFINITY, 0.f);
 }
 
 // four values to consecutive elements of an output row
@@ -81,6 +85,7 @@ __device__ __forceinline__ void store4(bf16_t *p, f4 v) {
 template <int DH, int NW, typename TI, typename TO>
 __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void prompt_kernel(PromptArgs pa) {
     constexpr int QP = sizeof(TI) == 4 ? 3 : 1, PP = sizeof(TO) == 4 ? 2 : 1;
+    constexpr float RAISE = Slack<TO>::raise, SHIFT = Slack<TO>::shift;
     constexpr int NK = DH / 16, ND = DH / 32;           // contraction steps of S, tiles of 32 output columns
     constexpr int NTHR = 64 * NW, TPR = DH / 16;        // threads per row of codes (16 each)
     constexpr int NL = BLK * TPR / NTHR < 1 ? 1 : BLK * TPR / NTHR;   // 16-byte loads per thread
@@ -324,7 +329,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         };
         if (pa.nsplit == 1) {
             put((TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st);
-            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = weight_stat(ref.m, pad ? 0.f : l);
+            if (pa.stat && hi == 0) pa.stat[(size_t)si * R + r] = weight_stat(ref.m, pad ? 0.f : l, SHIFT);
         } else {
             const size_t at = ((size_t)si * pa.nsplit + split) * R + r;
             put(pa.part_o + at * DH);
@@ -354,7 +359,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs pa) {
     TO *op = (TO *)a.out + b * a.q_sb + hq * a.q_sh + t * a.q_st;
 #pragma unroll
     for (int e = 0; e < 4; e++) stf(op, col + e, L == 0.f ? 0.f : acc[e] / L);
-    if (pa.stat && col == 0) pa.stat[(size_t)si * R + r] = weight_stat(mu, L);
+    if (pa.stat && col == 0) pa.stat[(size_t)si * R + r] = weight_stat(mu, L, Slack<TO>::shift);
 }
 
 // sum over the 32 lanes of a half wavefront, in each of them

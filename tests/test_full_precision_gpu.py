@@ -98,3 +98,28 @@ def test_distance_of_gathered_weights(d, dtype):
         off = fd.distance(c.weight[:, :, :n], want[:, :, :n])
         print(f"weights d {d} {dtype} {(Hq, Hkv, cap, held, T)}: {off:.3g}", flush=True)
         assert off <= (1e-6 if T < 10 else 1.5e-7), (Hq, Hkv, cap, held, T, off)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype,out,below", [("bf16", "f32", 17), ("f32", "f32", 17), ("bf16", "bf16", 26)])
+def test_small_weights_beside_a_large_one_without_value(d, dtype, out, below):
+    """A sink: one pair takes nearly all of the weight and has the value zero, so that a row's output is made of weights of 2^-17 (2^-26) alone.  fp32
+    outputs: a logit of 17 is off by 3 roundings of 2^-24 of it (the scale's two and its own), 2.2e-6 of the weights, their own two parts by 2^-21 at
+    most: 3e-6 in all.  bf16 outputs: the rounding of the result and 2^-10 for the weights."""
+    for B, Hq, cap, held, T in ((256, 2, 1088, 1000, 1), (2, 4, 4096, 3000, 1), (256, 20, 1088, 1000, 1), (2, 4, 1088, 1000, 4), (2, 4, 4096, 3000, 100), (128, 4, 1088, 900, 100)):
+        rng = np.random.default_rng(d + T)
+        c = lb.LolaFullCache(B, Hq, 1, d, cap, dtype=dtype, out_dtype=out, device=DEV)
+        n = held + T
+        k, v = (tokens(rng, (1, 1, n, d), dtype, gain).repeat(B, 1, 1, 1) for gain in (0.3, 1.0))
+        k[..., 0] = 0.0
+        k[:, :, 5] = 0.0
+        k[:, :, 5, 0] = 8.0
+        v[:, :, 5] = 0.0
+        c.append(k, v)
+        q = tokens(rng, (B, Hq, T, d), dtype, 1.0)
+        q[..., 0] = below * math.log(2.0) * math.sqrt(d) / 8.0
+        y = c.attend(q).double()
+        want, _ = fd.attend(c, q)
+        off = fd.distance(y, want)
+        print(f"small weights d {d} {dtype}->{out} {(B, Hq, cap, held, T)}: {off:.3g}", flush=True)
+        assert off <= (3e-6 if out == "f32" else NORM[out] + 2.0 ** -10), (B, Hq, cap, held, T, off)
