@@ -23,6 +23,31 @@ def tokens(rng, shape, dtype, gain=1.0):
     return torch.from_numpy(rng.standard_normal(shape).astype(np.float32) * np.float32(gain)).to(TORCH[dtype]).to(DEV)
 
 
+# Hq, Hkv, capacity, pairs held before, new tokens: step in one workgroup, in shares, two column tiles; few rows, in two tiles; many rows in one
+# share, in several
+FORMS = [(4, 2, 192, 150, 1), (8, 1, 4096, 3000, 1), (20, 1, 2048, 900, 1), (4, 1, 2048, 1000, 4), (8, 2, 2048, 500, 5), (4, 2, 512, 0, 300), (8, 2, 4096, 2000, 70)]
+
+
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
+def test_distance_from_64_bits(d, dtype, out):
+    for Hq, Hkv, cap, held, T in FORMS:
+        rng = np.random.default_rng(d + held)
+        c = lb.LolaFullCache(2, Hq, Hkv, d, cap, dtype=dtype, out_dtype=out, device=DEV)
+        if held:
+            c.append(tokens(rng, (2, Hkv, held, d), dtype, 1.3), tokens(rng, (2, Hkv, held, d), dtype))
+        q, k, v = tokens(rng, (2, Hq, T, d), dtype), tokens(rng, (2, Hkv, T, d), dtype, 1.3), tokens(rng, (2, Hkv, T, d), dtype)
+        if T > 1:
+            c.append(k, v)
+            y = c.attend(q)
+        else:
+            y = c.step(*(x[:, :, 0].contiguous() for x in (q, k, v)))[:, :, None]
+        want, _ = fd.attend(c, q)
+        off = fd.distance(y, want)
+        print(f"outputs d {d} {dtype}->{out} {(Hq, Hkv, cap, held, T)}: {off:.3g}", flush=True)
+        assert off <= NORM[out], (Hq, Hkv, cap, held, T, off)
+
+
 @pytest.mark.parametrize("d", [32, 64, 128, 256])
 @pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f32", "f32")])
 def test_huge_values_of_pairs_without_weight(d, dtype, out):
