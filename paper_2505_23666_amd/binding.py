@@ -433,7 +433,8 @@ class LolaFullCache:
         lola_full_append(self.cfg, self.st, k, v, lens, T)
 
     def attend(self, q, lens=None, out=None, gather=False):
-        """Outputs of the newest tokens' queries q [B, Hq, T, d] ([B, T, Hq, d]); gather adds their weights to `weight`."""
+        """Outputs of the newest tokens' queries q [B, Hq, T, d] ([B, T, Hq, d]); gather adds their weights to `weight`.
+        out may be q where their types are alike, without gather."""
         T = self._tokens(q, self.Hq)
         self._lens(lens)
         out = self._out(out, q.shape)

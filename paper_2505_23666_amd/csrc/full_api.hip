@@ -12,6 +12,7 @@ namespace {
 
 constexpr size_t ALIGN = 256;
 inline size_t up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+inline int bytes_of(int32_t dtype) { return dtype == LOLA_F32 ? 4 : 2; }
 inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 #define LAUNCH_CHECK() do { if (hipGetLastError() != hipSuccess) return LOLA_ERR_HIP; } while (0)
 
@@ -254,6 +255,18 @@ lola_status check_attend(const lola_full_config *c, const lola_full_state *st, c
     return LOLA_OK;
 }
 
+// Every row's output is written by the workgroup that alone reads its query, after that, or by a later launch: outputs may lie in the queries' place.  Not so
+// where weights are gathered, whose kernel reads the queries again.  k, v: NULL, or a step's token.
+lola_status check_overlap(const lola_full_config *c, const void *q, const void *k, const void *v, int32_t T, int32_t gather, const void *out) {
+    auto overlap = [&](const void *x, int heads) {
+        const uintptr_t a = (uintptr_t)x, o = (uintptr_t)out, row = (uintptr_t)c->batch * T * c->head_dim;
+        return a < o + row * c->n_q_heads * bytes_of(c->out_dtype) && o < a + row * heads * bytes_of(c->dtype);
+    };
+    if (overlap(q, c->n_q_heads) && (q != out || c->dtype != c->out_dtype || gather)) return LOLA_ERR_UNSUPPORTED;
+    if (k && (overlap(k, c->n_kv_heads) || overlap(v, c->n_kv_heads))) return LOLA_ERR_UNSUPPORTED;
+    return LOLA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -307,6 +320,8 @@ lola_status lola_full_attend(const lola_full_config *c, const lola_full_state *s
     rc = check_attend(c, st, q, T, gather, out, workspace, workspace_bytes);
     if (rc != LOLA_OK) return rc;
     if (lens && misaligned(lens)) return LOLA_ERR_ALIGN;
+    rc = check_overlap(c, q, nullptr, nullptr, T, gather, out);
+    if (rc != LOLA_OK) return rc;
     return attend(c, st, q, nullptr, nullptr, lens, T, gather, out, workspace, (hipStream_t)stream);
 }
 
@@ -321,6 +336,8 @@ lola_status lola_full_step(const lola_full_config *c, const lola_full_state *st,
     rc = check_attend(c, st, q, 1, gather, out, workspace, workspace_bytes);
     if (rc != LOLA_OK) return rc;
     if (misaligned(k) || misaligned(v)) return LOLA_ERR_ALIGN;
+    rc = check_overlap(c, q, k, v, 1, gather, out);
+    if (rc != LOLA_OK) return rc;
     if (plan_attend(c, 1, gather).step) return attend(c, st, q, k, v, nullptr, 1, gather, out, workspace, (hipStream_t)stream);
     rc = append(c, st, k, v, nullptr, 1, (hipStream_t)stream);      // more query heads per kv head than the step kernel takes
     if (rc != LOLA_OK) return rc;
