@@ -78,10 +78,11 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
     size_t off = 0;
     if (p.step) {
         // Two workgroups per compute unit, which all run at once (8 streams of 128 Ki pairs at d = 128 54.4 us a step with the join, 56.9 with four; 8
-        // of 32 Ki 19.8 and 22.6; but 128 streams of unequal lengths up to 8192 with weights 61.7 and 60.3), and shares of at most 8192 slots
-        // (sequences of unequal lengths); each wavefront has a block at least when the cache is full.
+        // of 32 Ki 19.8 and 22.6; but 128 streams of unequal lengths up to 8192 with weights 61.7 and 60.3), and shares of about 8192 slots
+        // (sequences of unequal lengths), 16320 at most: 255 blocks, STEP_BLOCKS for each of four wavefronts; each wavefront has a block at least when the cache is full.
         const size_t most = ((size_t)c->capacity / BLK + 3) / 4;
         p.nsplit = (int)std::max((size_t)1, std::min(most, std::max((2 * CHIP_CUS + S - 1) / S, (size_t)c->capacity / 8192)));
+        static_assert(2 * 8192 / BLK <= 4 * STEP_BLOCKS, "a share of less than twice 8192 slots");
         // One workgroup of eight wavefronts per stream, and no join, where the streams fill the chip (256 streams of 4096 pairs at
         // d = 128 46 us a step, 50 in four shares each; 512 streams 105 and 108; but 128 streams of up to 8192 pairs 80 and 66) or the cache is
         // short (8 streams of 512 slots at d = 64 5.7 us, joined 7.0; but 1024 slots 7.1 and 6.8).

@@ -30,6 +30,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i2 __attribute__((ext_vector_type(2)));
 
 constexpr float P_SHIFT = 14.f;    // probabilities are held times 2^14
+constexpr int STEP_BLOCKS = 64;    // most blocks that one wavefront of the step kernel reads
 
 // eight codes times their block's scale -> eight bf16 (exact: the keys themselves)
 __device__ __forceinline__ bf8 codes_to_bf16(uint32_t a, uint32_t b, float scale) {
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
     const int64_t pos0 = MASK ? a.mem.n_tokens[si] - n : 0;
 
     uint32_t kr[4][KB / 4], vr[VI * 4];
-    float ksT = 0.f, vsT = 0.f;       // scales of this wavefront's next 64 blocks, one per lane (a scalar load would make each LDS wait longer)
+    float ksT = 0.f, vsT = 0.f;       // scales of this wavefront's blocks, 64 at most (STEP_BLOCKS), one per lane (a scalar load would make each LDS wait longer)
     auto scales = [&](int J) {
         const int x = min(J + NW * lane, a.nblk - 1);
         ksT = ks[x]; vsT = vs[x];
@@ -282,7 +283,6 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
     uint8_t *st = stage[w];
     const float minus_one = opaque_minus_one();
     for (int J = J0 + w, it = 0; J < J1; J += NW, it++) {
-        if (it == 64) { it = 0; scales(J); }
         const float ksJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksT), it)), vsJ = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsT), it));
         const int live = count - J * BLK;          // slots of this block that hold pairs (64 and more: all)
         const float c = a.scale2, ev = (float)exponent_of(vsJ);
