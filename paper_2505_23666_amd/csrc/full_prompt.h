@@ -161,7 +161,6 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         if (t < n) load_query((const TI *)a.q + b * a.q_sb + hq * a.q_sh + t * a.q_st + s * 16 + hi * 8, qf[s]);
         else zero_query<QP>(qf[s]);
     }
-    if constexpr (QP == 1) spoil_query<NK>(qf[0]);
     f16v o[ND];
 #pragma unroll
     for (int d = 0; d < ND; d++)
@@ -206,12 +205,22 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
     const float c = a.scale2;
     const float minus_one = opaque_minus_one();
     float ev = 0.f;      // exponent of the staged block's values
-    bool masked = false;
+    bool masked = false, far = false;      // far: of any row (references only change where they are moved)
     if (J < J1) {
         load(J);
         ev = (float)exponent_of(lane_of_f(vsT, J));
         masked = (int64_t)lane_of(spT.y, J) > w_first;
         store(lds, J, lane_of_f(ksT, J));
+    }
+    if constexpr (QP == 1) {
+        f16v sum;
+#pragma unroll
+        for (int e = 0; e < 16; e++) sum[e] = 0.f;
+        bf8 zero;
+        zero_query<1>(&zero);
+#pragma unroll
+        for (int k = 0; k < NK; k++) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zero, qf[k][0], sum, 0, 0, 0);
+        spoil_query(qf[0], sum[0]);
     }
     lds_barrier();
     auto block = [&](auto which) {
@@ -252,21 +261,23 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
 #pragma unroll
             for (int e = 0; e < 16; e++) mb = fmaxf(mb, s[kt][e]);
         mb *= c;
-        if (__any(mb - ref.m > RAISE + fminf(ref.x - ev, 0.f))) {
+        if (__builtin_expect(__any(mb - ref.m > RAISE + fminf(ref.x - ev, 0.f)), 0)) {
             float fl, fo;
             ref.move(half_max(mb), ev, fl, fo);
+            far = __any(ref.far());
             l *= fl;
 #pragma unroll
             for (int d = 0; d < ND; d++) o[d] *= fo;
         }
         const float drop = ref.drop(ev);
-        float cs = c, off = ref.m + (drop - SHIFT);
-        if (__any(ref.far())) {
-            cs = 1.f; off = drop - SHIFT;
+        float off = ref.m + (drop - SHIFT);
+        if (__builtin_expect(far, 0)) {
+            off = drop - SHIFT;
+            const float ic = 1.f / c;
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) s[kt][e] = fmaf(s[kt][e], c, -ref.m);
+                for (int e = 0; e < 16; e++) s[kt][e] = fmaf(s[kt][e], c, -ref.m) * ic;
         }
         h8 pf[4][PP];
         float sum = 0.f;
@@ -274,7 +285,7 @@ __global__ __launch_bounds__(64 * NW, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) vo
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[kt][e], cs, -off)), y = __builtin_amdgcn_exp2f(fmaf(s[kt][e + 1], cs, -off));
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[kt][e], c, -off)), y = __builtin_amdgcn_exp2f(fmaf(s[kt][e + 1], c, -off));
                 sum += x; sum += y;
                 h2 part[PP];
                 to_f16_parts<PP>(x, y, minus_one, part);

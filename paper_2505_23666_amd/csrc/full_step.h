@@ -128,18 +128,11 @@ __device__ __forceinline__ void load_query(const float *p, bf8 *part) {
     split_bf16(x, part);
 }
 // A query with an element that is not finite has the output NaN wherever it sees a pair: an infinite element makes each of its logits infinite
-// or NaN, and a softmax of infinities is NaN, also where all of them are negative and would pass for weights of zero.  So one such element
-// among a lane's N operands makes the first operand NaN, and with it every logit of the row.  (Two elements at a time: an exponent of
-// ones carries into the sign's place.)
-template <int N>
-__device__ __forceinline__ void spoil_query(bf8 *q) {
-    uint32_t carry = 0;
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const uint4 u = __builtin_bit_cast(uint4, q[i]);
-        carry |= ((u.x & 0x7F807F80u) + 0x00800080u) | ((u.y & 0x7F807F80u) + 0x00800080u) | ((u.z & 0x7F807F80u) + 0x00800080u) | ((u.w & 0x7F807F80u) + 0x00800080u);
-    }
-    if (carry & 0x80008000u) q[0] = __builtin_bit_cast(bf8, make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u));
+// or NaN, and a softmax of infinities is NaN, also where all of them are negative and would pass for weights of zero.  So `sum`, the row's
+// product with zeros (NaN for such a query, else 0), makes its first operand NaN, and with it every logit.  (A test of the elements would move
+// all operands through vector registers: many rows at d = 256 took 14 % longer.)
+__device__ __forceinline__ void spoil_query(bf8 *q, float sum) {
+    if (__any(sum != 0.f) && sum != 0.f) q[0] = __builtin_bit_cast(bf8, make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u));
 }
 template <int QP>
 __device__ __forceinline__ void zero_query(bf8 *part) {
@@ -269,7 +262,14 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
             if (t < n) load_query(qp + (DH == 32 ? quad * 8 : (s / 2) * 64 + quad * 16 + (s & 1) * 8), qf[ct][s]);
             else zero_query<QP>(qf[ct][s]);
         }
-        if constexpr (QP == 1) spoil_query<NK>(qf[ct][0]);
+        if constexpr (QP == 1) {
+            f4 sum = {0.f, 0.f, 0.f, 0.f};
+            bf8 zero;
+            zero_query<1>(&zero);
+#pragma unroll
+            for (int s = 0; s < NK; s++) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zero, qf[ct][s][0], sum, 0, 0, 0);
+            spoil_query(qf[ct][0], sum[0]);
+        }
     }
     f4 o[CT][ND];
     RowRef ref[CT];
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(64 * NW) void step_kernel(StepArgs sa) {
             ref[ct].move(quad_max(mb), ev, fl, fo);
             const float t = ref[ct].drop(ev);
             float off = ref[ct].m + (t - P_SHIFT);
-            if (__any(ref[ct].far())) {
+            if (__builtin_expect(__any(ref[ct].far()), 0)) {
                 off = t - P_SHIFT;
 #pragma unroll
                 for (int k = 0; k < 4; k++)
