@@ -370,7 +370,10 @@ class LolaFullCache:
 
     def reset(self):
         """Empty caches."""
-        self._on_device(lola_full_init, self.cfg, self.st)
+        self._on_device(self._reset)
+
+    def _reset(self):
+        lola_full_init(self.cfg, self.st)
         self._shrunk(0)
 
     def _shrunk(self, fill):
@@ -460,5 +463,8 @@ class LolaFullCache:
 
     def evict(self, keep, first=0, recent=0):
         """Cut every stream to `keep` pairs: the first `first` and the most recent `recent` tokens, then those of largest weight."""
-        self._on_device(lola_full_evict, self.cfg, self.st, int(keep), int(first), int(recent), self._ws(0, 0))
-        self._shrunk(int(keep))
+        self._on_device(self._evict, int(keep), int(first), int(recent))
+
+    def _evict(self, keep, first, recent):
+        lola_full_evict(self.cfg, self.st, keep, first, recent, self._ws(0, 0))
+        self._shrunk(keep)
