@@ -292,6 +292,7 @@ lola_status lola_full_init(const lola_full_config *cfg, const lola_full_state *s
  * A token with an element that is not finite is stored with NaN in place of its whole key, and zeros for those elements of its value:
  * every query that sees it gets NaN, no other does.
  * Tokens beyond `capacity` are not stored: count stays at capacity, n_tokens counts them.
+ * Token indices are int32: n_tokens must stay below 2^31.  Elements above 1.9375 x 2^127 in size round to 2^128, which fp32 does not hold.
  */
 lola_status lola_full_append(const lola_full_config *cfg, const lola_full_state *st, const void *k, const void *v,
                              const int32_t *lens, int32_t T, void *stream);
@@ -301,7 +302,8 @@ lola_status lola_full_append(const lola_full_config *cfg, const lola_full_state 
  * the pairs whose idx is at most that.  All query heads of a group read the same cache:
  *   y_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j) / sum_j exp(scale q_i.k_j).
  * A query that sees nothing, and the rows i >= n, get zeros.  A query with an element that is not finite gets NaN if it sees anything.
- * (Terms below 2^-36 of the largest product of a weight that the row gives and 448 times the scale of that pair's block may be lost.)
+ * (Terms below 2^-36 of the largest product of a weight that the row gives and 448 times the scale of that pair's block may be lost, and weights below 2^-126;
+ * logits beyond fp32 are infinite.)
  * gather = 1 adds sum over the group's query heads and i < n of p_ij to weight[j]; queries whose output is NaN add nothing.
  * q, out [B, Hq, T, d] (or tokens first).  out may be q where their types are alike and gather = 0; any other overlap of out with q (lola_full_step: and
  * with k, v) is refused with LOLA_ERR_UNSUPPORTED.  T >= 0; T * (Hq / Hkv) at most 2^24, B * Hq * T at most 2^30 (also in lola_full_append).

@@ -77,9 +77,11 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
     p.step = R <= step_rows(c->head_dim);
     size_t off = 0;
     if (p.step) {
-        // Two workgroups per compute unit, which all run at once (8 streams of 128 Ki pairs at d = 128 54.4 us a step with the join, 56.9 with four; 8
-        // of 32 Ki 19.8 and 22.6; but 128 streams of unequal lengths up to 8192 with weights 61.7 and 60.3), and shares of about 8192 slots
-        // (sequences of unequal lengths), 16320 at most: 255 blocks, STEP_BLOCKS for each of four wavefronts; each wavefront has a block at least when the cache is full.
+        // Two workgroups per compute unit (8 streams of 128 Ki pairs at d = 128 54.4 us a step with the join, 56.9 with four; 8 of 32 Ki 19.8 and 22.6; but 128
+        // streams of unequal lengths up to 8192 with weights 61.7 and 60.3).  All run at once in the forms that these figures are of: one token, up to 16 rows,
+        // d up to 128, bf16 storage or outputs.  The registers of others leave room for one (fp32 storage and outputs at d = 128, several tokens at d = 128,
+        // more than 16 rows at d = 128 and, with several tokens or fp32 storage, at d = 64; d = 256): half of those shares wait for the others.  Shares have about 8192
+        // slots (sequences of unequal lengths), 16320 at most: 255 blocks, STEP_BLOCKS for each of four wavefronts; each wavefront has a block at least when the cache is full.
         const size_t most = ((size_t)c->capacity / BLK + 3) / 4;
         p.nsplit = (int)std::max((size_t)1, std::min(most, std::max((2 * CHIP_CUS + S - 1) / S, (size_t)c->capacity / 8192)));
         static_assert(2 * 8192 / BLK <= 4 * STEP_BLOCKS, "a share of less than twice 8192 slots");
@@ -94,7 +96,7 @@ AttendPlan plan_attend(const lola_full_config *c, int32_t T, int32_t gather) {
         p.off_counts = off; if (gather) off += up(S * 4);
     } else {
         p.ntiles = (int)((R + 32 * PROMPT_NW - 1) / (32 * PROMPT_NW));
-        // two workgroups fit a compute unit; fewer are split over the blocks, four blocks each at least when the cache is full
+        // two workgroups fit a compute unit (one with fp32 queries at d = 128, and at d = 256); fewer are split over the blocks, four blocks each at least when the cache is full
         const size_t wgs = S * p.ntiles, most = std::max((size_t)1, (size_t)c->capacity / BLK / 4);
         p.nsplit = (int)(wgs >= 2 * CHIP_CUS ? 1 : std::min(most, (2 * CHIP_CUS + wgs - 1) / wgs));
         // (a launch of its own, 3 us, against 16 loads per lane in every workgroup: at 5 blocks a call of 27 us takes 23 without it, at 64

@@ -9,10 +9,11 @@
 // transposing 16-bit LDS read.  Which blocks can be passed over and which need a comparison per element follows from the least and largest token
 // index of each block (of long caches taken beforehand by a kernel of its own): slots need not be in the order of tokens (evictions fill holes).
 //
-// Bound by the sum of its matrix and vector instructions, of two wavefronts per SIMD, and by power: four prompts of 4096 tokens (32 query, 8 kv
-// heads, d = 128, bf16) 0.61 ms alone, 900 TFLOP/s, where a large library product reaches 1330; the same with all elements equal is a fifth
+// Bound by the sum of its matrix and vector instructions, of two wavefronts per SIMD, by LDS, as busy as the matrix cores (every wavefront reads all of a block for its
+// 32 rows; a quarter of the active cycles are bank conflicts), and by power: four prompts of 4096 tokens (32 query, 8 kv heads, d = 128, bf16) 0.59 ms in a long row of
+// passes, 930 TFLOP/s, 0.68 to 0.8 ms in the first twenty, where a large library product reaches 1330; the same with all elements equal is a fifth
 // faster.  A block of a wavefront is 32 products of 32 cycles, 32 exponentials, about 200 other vector instructions and 32 KB from LDS.  At
-// d = 64 the exponentials weigh as much as the products (two prompts of 2000 tokens, fp32 outputs: 70 us).
+// d = 64 the exponentials weigh as much as the products (two prompts of 2000 tokens, fp32 outputs: 72 us).
 //
 // The row's references (RowRef) are only moved when a logit exceeds them by more than `raise`: weights (times scales) then reach 2^raise, held times
 // 2^shift in fp16 (Slack).
@@ -35,7 +36,7 @@ template <typename TO> struct Slack { static constexpr float raise = sizeof(TO) 
 struct PromptArgs {
     Args a;
     int nsplit, ntiles;
-    int2 *span;        // [S][nblk] least and largest token index of each block; NULL: up to 64 blocks, each workgroup looks at the indices
+    int2 *span;        // [S][nblk] least and largest token index of each block; NULL: up to 16 blocks, each workgroup looks at the indices
     float *part_o;     // [S][nsplit][R][d] outputs of the shares, normalised
     float *part_ml;    // [S][nsplit][R][2] RowRef::m and sum
     float2 *stat;      // [S][R] weight_stat(), where weights are gathered
@@ -382,7 +383,8 @@ __device__ __forceinline__ float sum32(float v) {
 
 // weight[j] += sum over rows of their weight of pair j (weight_stat): one workgroup per block of slots, whose keys stay in registers as the first operand of
 // S^T = K Q^T; the wavefronts take 32 rows in turn, straight from global memory, and join their sums at the end.  Bound by vector
-// instructions: an exponential and three others per logit (two prompts of 2000 tokens at d = 64: 57 us, 16.4 GFLOP).
+// instructions, an exponential and three others per logit, and by unequal workgroups: the first block's has all rows, the last one's hardly any (two prompts of
+// 2000 tokens at d = 64: 58 us, 16.4 GFLOP).
 template <int DH, typename TI>
 __global__ __launch_bounds__(256, (DH == 256 || sizeof(TI) == 4) ? 1 : 2) void prompt_gather_kernel(PromptArgs pa) {
     constexpr int QP = sizeof(TI) == 4 ? 3 : 1, NK = DH / 16;
