@@ -305,8 +305,8 @@ lola_status lola_full_append(const lola_full_config *cfg, const lola_full_state 
  * (Terms below 2^-36 of the largest product of a weight that the row gives and 448 times the scale of that pair's block may be lost, and weights below 2^-126;
  * logits beyond fp32 are infinite.)
  * gather = 1 adds sum over the group's query heads and i < n of p_ij to weight[j]; queries whose output is NaN add nothing.
- * q, out [B, Hq, T, d] (or tokens first).  out may be q where their types are alike and gather = 0; any other overlap of out with q (lola_full_step: and
- * with k, v) is refused with LOLA_ERR_UNSUPPORTED.  T >= 0; T * (Hq / Hkv) at most 2^24, B * Hq * T at most 2^30 (also in lola_full_append).
+ * q, out [B, Hq, T, d] (or tokens first).  out may be q where their types are alike, with gather = 1 only up to T * (Hq / Hkv) = 32 (16 at head_dim 256); any
+ * other overlap of out with q (lola_full_step: and with k, v) is refused with LOLA_ERR_UNSUPPORTED.  T >= 0; T * (Hq / Hkv) at most 2^24, B * Hq * T at most 2^30 (also in lola_full_append).
  */
 lola_status lola_full_attend(const lola_full_config *cfg, const lola_full_state *st, const void *q, const int32_t *lens,
                              int32_t T, int32_t gather, void *out, void *workspace, size_t workspace_bytes, void *stream);

@@ -437,7 +437,7 @@ class LolaFullCache:
 
     def attend(self, q, lens=None, out=None, gather=False):
         """Outputs of the newest tokens' queries q [B, Hq, T, d] ([B, T, Hq, d]); gather adds their weights to `weight`.
-        out may be q where their types are alike, without gather."""
+        out may be q where their types are alike (with gather only for few rows, see lola.h)."""
         T = self._tokens(q, self.Hq)
         self._lens(lens)
         out = self._out(out, q.shape)

@@ -259,13 +259,13 @@ lola_status check_attend(const lola_full_config *c, const lola_full_state *st, c
 }
 
 // Every row's output is written by the workgroup that alone reads its query, after that, or by a later launch: outputs may lie in the queries' place.  Not so
-// where weights are gathered, whose kernel reads the queries again.  k, v: NULL, or a step's token.
+// where the weights of many rows are gathered, whose kernel reads the queries again.  k, v: NULL, or a step's token.
 lola_status check_overlap(const lola_full_config *c, const void *q, const void *k, const void *v, int32_t T, int32_t gather, const void *out) {
     auto overlap = [&](const void *x, int heads) {
         const uintptr_t a = (uintptr_t)x, o = (uintptr_t)out, row = (uintptr_t)c->batch * T * c->head_dim;
         return a < o + row * c->n_q_heads * bytes_of(c->out_dtype) && o < a + row * heads * bytes_of(c->dtype);
     };
-    if (overlap(q, c->n_q_heads) && (q != out || c->dtype != c->out_dtype || gather)) return LOLA_ERR_UNSUPPORTED;
+    if (overlap(q, c->n_q_heads) && (q != out || c->dtype != c->out_dtype || (gather && !plan_attend(c, T, gather).step))) return LOLA_ERR_UNSUPPORTED;
     if (k && (overlap(k, c->n_kv_heads) || overlap(v, c->n_kv_heads))) return LOLA_ERR_UNSUPPORTED;
     return LOLA_OK;
 }

@@ -32,20 +32,21 @@ def test_overlaps_are_refused(L, dtype, out_dtype):
         nq, no = size(8, T, dtype), size(8, T, out_dtype)
         for gather in (0, 1):
             assert att(BASE, BASE + 16, T, gather) == att(BASE, BASE + nq - 16, T, gather) == att(BASE, BASE - no + 16, T, gather) == -5
-            if gather or dtype != out_dtype:
+            if (gather and T == 100) or dtype != out_dtype:
                 assert att(BASE, BASE, T, gather) == -5
     nq, nk, no = size(8, 1, dtype), size(2, 1, dtype), size(8, 1, out_dtype)
     clear = 0x10000
     assert stp(BASE, BASE + clear, BASE + 2 * clear, BASE + 16) == stp(BASE, BASE + clear, BASE + 2 * clear, BASE + nq - 16) == -5
     assert stp(BASE, BASE + clear, BASE + 2 * clear, BASE + clear) == stp(BASE, BASE + clear, BASE + 2 * clear, BASE + clear + nk - 16) == -5
     assert stp(BASE, BASE + clear, BASE + 2 * clear, BASE + 2 * clear) == stp(BASE, BASE + clear, BASE + 2 * clear, BASE + 2 * clear - no + 16) == -5
-    assert stp(BASE, BASE + clear, BASE + 2 * clear, BASE, 1) == -5
+    c.n_q_heads = 66      # 33 query heads per kv head: the kernels of many rows, also in a step
+    assert att(BASE, BASE, 1, 1) == stp(BASE, BASE + 16 * clear, BASE + 32 * clear, BASE, 1) == -5
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_outputs_in_the_queries_place(dtype):
-    """Without weights the outputs may take the queries' place: the same bits as beside them, in every kernel; with weights the call is refused."""
+    """The outputs may take the queries' place: the same bits as beside them, in every kernel; with weights over many rows the call is refused."""
     dt, dev = (torch.bfloat16 if dtype == "bf16" else torch.float32), "cuda:0"
     rng = np.random.default_rng(1)
     x = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(dt).to(dev)  # noqa: E731
@@ -61,8 +62,17 @@ def test_outputs_in_the_queries_place(dtype):
         place = q.clone()
         assert c.attend(place, out=place) is place
         assert torch.equal(place, want), (Hq, d, cap, held, T)
-        with pytest.raises(lb.LolaError, match="no kernel"):
-            c.attend(q, out=q, gather=True)
+        if T * Hq // 2 > (16 if d == 256 else 32):
+            with pytest.raises(lb.LolaError, match="no kernel"):
+                c.attend(q, out=q, gather=True)
+        else:
+            c.weight.zero_()
+            want, weight = c.attend(q, gather=True), c.weight.clone()
+            c.weight.zero_()
+            place = q.clone()
+            c.attend(place, out=place, gather=True)
+            n = held + T
+            assert torch.equal(place, want) and torch.equal(c.weight[:, :, :n], weight[:, :, :n]), (Hq, d, cap, held, T)
     assert c.step(*(t[:, :, 0].contiguous() for t in (q, k, v))).shape == (2, 2, 256)
     q1, k1, v1 = (t[:, :, 0].contiguous() for t in (q, k, v))
     with pytest.raises(lb.LolaError):
